@@ -1,0 +1,128 @@
+/*
+ * dropcompute_train.h — C ABI of the training operators that go with the threshold sweep, for NVIDIA B200 (sm_100a).
+ *
+ * DropCompute (arXiv 2306.10598, Algorithm 1) lets a worker accumulate the gradients of its micro-batches until the
+ * threshold tau has passed; dropcompute.h says which tau to take.  The operators here compute the parts of a language
+ * model's micro-batch that depend on the vocabulary (lookup, loss and their gradients, accumulated over as many
+ * micro-batches as were run) and keep its activations in 8 bits, which is what sets the size of a micro-batch.
+ *
+ * Conventions are those of dropcompute.h: DEVICE pointers unless stated, work is enqueued on `stream` and the call
+ * returns, nothing is allocated, nothing is kept between calls, any number of host threads may call at once, every
+ * function returns a dc_status, and what the host can see to be wrong returns an error and enqueues nothing.  Two calls on
+ * the same inputs give the same bits.  Matrices are row-major with a row stride in ELEMENTS (at least the row length; the
+ * elements of a row are adjacent).  Any alignment and any stride is accepted unless stated; rows that start on 16-byte
+ * boundaries take the fastest path.  Outputs must not overlap inputs.
+ *
+ * Element types: DC_BF16, DC_F16, DC_F32.
+ */
+#ifndef DROPCOMPUTE_TRAIN_H_
+#define DROPCOMPUTE_TRAIN_H_
+
+#include "dropcompute.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define DC_BF16 0
+#define DC_F16 1
+#define DC_F32 2
+
+/*
+ * dc_embed — embedding lookup with scaling:   out[n][:] = round( scale * table[ids[n]][:] )
+ *
+ *   table      [V][D] of `dtype`, row stride table_stride       ids   [N] int64       out   [N][D] of `dtype`, out_stride
+ *   pad_id     rows whose id equals it are zeros; a negative pad_id matches nothing
+ *   N >= 0 (0 enqueues nothing), V > 0, D > 0.  An id outside [0, V) gives a row of NaN; no memory is read for it.
+ */
+int dc_embed(const void *table, int64_t table_stride, int32_t dtype, const int64_t *ids, int64_t N, int64_t V, int64_t D,
+             float scale, int64_t pad_id, void *out, int64_t out_stride, void *stream);
+
+/*
+ * dc_embed_backward — the gradient of dc_embed with respect to the table:
+ *
+ *   dtable[v][:] = (accumulate ? dtable[v][:] : 0) + scale * sum over n with ids[n] = v of dout[n][:]
+ *
+ * The sum is taken in fp32 in a fixed order and rounded once to dtable_dtype, which is `dtype` or DC_F32.  Tokens that are
+ * pad_id or outside [0, V) contribute nothing.  With accumulate = 0 every row of dtable is written; with accumulate = 1
+ * only rows of tokens that occur are read and written.  N = 0 is allowed.  V <= DC_EMBED_MAX_V, N, D <= 2^30.
+ *   workspace  at least dc_embed_backward_workspace_bytes(N, V, D) bytes, 256-byte aligned
+ */
+#define DC_EMBED_MAX_V 4194304
+size_t dc_embed_backward_workspace_bytes(int64_t N, int64_t V, int64_t D);
+int dc_embed_backward(const void *dout, int64_t dout_stride, int32_t dtype, const int64_t *ids, int64_t N, int64_t V, int64_t D,
+                      float scale, int64_t pad_id, void *dtable, int64_t dtable_stride, int32_t dtable_dtype, int32_t accumulate,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dc_gelu_save8 — y = gelu(x), and x kept in 8 bits for the backward pass.
+ *
+ *   gelu(x) = x / (1 + exp(-2u)),  u = sqrt(2/pi) (x + 0.044715 x^3)   (the tanh form)
+ *
+ * Per group of DC_SAVE8_GROUP neighbours of a row (the last group of a row may be shorter), a = max |x|:
+ *   scale = fl32(a * fl32(1/127)),  q = round-to-even( fl32(x * fl32(127 / a)) ), an integer in [-127, 127];  a <= 2^-100: scale = q = 0.
+ * A group that holds an infinity or a NaN gets scale = NaN: what is read back from it is NaN.
+ *   x [N][D] of `dtype`, x_stride     y [N][D] of `dtype`, y_stride     q [N][D] int8, contiguous
+ *   scales [N][ceil(D / DC_SAVE8_GROUP)] fp32, contiguous       N >= 0, D > 0
+ */
+#define DC_SAVE8_GROUP 128
+int dc_gelu_save8(const void *x, int64_t x_stride, int32_t dtype, int64_t N, int64_t D, void *y, int64_t y_stride,
+                  int8_t *q, float *scales, void *stream);
+
+/*
+ * dc_gelu_save8_backward — the backward pass from the 8-bit values, x^ = fl32(q * scale):
+ *   dx = dy * gelu'(x^),   and, where y_again is not NULL, y_again = gelu(x^): the activation recomputed, for the weight
+ *   gradient of the layer behind it, so that neither x nor y is kept in 16 bits.
+ */
+int dc_gelu_save8_backward(const void *dy, int64_t dy_stride, int32_t dtype, const int8_t *q, const float *scales, int64_t N, int64_t D,
+                           void *dx, int64_t dx_stride, void *y_again, int64_t y_again_stride, void *stream);
+
+/*
+ * dc_vocab_loss — softmax cross entropy over a vocabulary, from the hidden states and the output weight, without the logits:
+ *
+ *   l[n][v] = logit_scale * sum_d hidden[n][d] * weight[v][d]        lse[n] = log sum_v exp l[n][v]
+ *   loss[n] = lse[n] - l[n][targets[n]]
+ *
+ * Rows with targets[n] == ignore_index have loss = lse = 0; whatever they hold (infinities and NaN too) is not used, and
+ * work is done for the labelled rows alone.  A target outside [0, V) that is not ignore_index gives loss = lse = NaN.
+ *   hidden [N][D], weight [V][D], both of `dtype`: DC_BF16 or DC_F16 (products on the tensor cores, sums in fp32)
+ *   targets [N] int64      loss, lse [N] fp32      N >= 0 (0 enqueues nothing), V, D > 0; N, V, D <= 2^30
+ *   workspace  at least dc_vocab_loss_workspace_bytes(...) bytes, 256-byte aligned
+ *
+ * dc_vocab_loss_workspace_bytes: backward = 0 for dc_vocab_loss, 1 for dc_vocab_loss_backward.  It depends on whether the
+ * weight's rows start on 16-byte boundaries (a copy is needed where they do not), hence `weight` and its stride.
+ */
+size_t dc_vocab_loss_workspace_bytes(int64_t N, int64_t V, int64_t D, const void *weight, int64_t weight_stride, int32_t backward);
+int dc_vocab_loss(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride, int32_t dtype,
+                  const int64_t *targets, int64_t N, int64_t V, int64_t D, int64_t ignore_index, float logit_scale,
+                  float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dc_vocab_loss_backward — its gradients.  With dloss[n] the gradient that arrives at loss[n]:
+ *
+ *   g[n][v]        = (exp(l[n][v] - lse[n]) - [v = targets[n]]) * dloss[n] * logit_scale      (0 for rows without a label)
+ *   dhidden[n][d]  = sum_v g[n][v] weight[v][d]                        (zeros for rows without a label)
+ *   dweight[v][d]  = (accumulate ? dweight[v][d] : 0) + sum_n g[n][v] hidden[n][d]
+ *
+ * The logits are computed again in pieces of the vocabulary, g is rounded to `dtype` for the two products (scaled by a
+ * power of two in DC_F16, so that small probabilities keep their bits), sums are taken in fp32.  Rows whose target is
+ * outside [0, V) contribute nothing.
+ *   lse, dloss [N] fp32, lse as dc_vocab_loss wrote it; values at rows without a label are not used
+ *   dhidden [N][D] of `dtype`, or NULL     dweight [V][D] of dweight_dtype (`dtype` or DC_F32), or NULL; not both NULL
+ */
+int dc_vocab_loss_backward(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride, int32_t dtype,
+                           const int64_t *targets, int64_t N, int64_t V, int64_t D, int64_t ignore_index, float logit_scale,
+                           const float *lse, const float *dloss, void *dhidden, int64_t dhidden_stride,
+                           void *dweight, int64_t dweight_stride, int32_t dweight_dtype, int32_t accumulate,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * dc_train_status — whether a bounded wait inside a kernel of this header expired on the current device since the last
+ * call (DC_ERR_DEVICE, and the mask in *flags, HOST, may be NULL); clears it.  Synchronises the device.
+ */
+int dc_train_status(uint32_t *flags);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* DROPCOMPUTE_TRAIN_H_ */

@@ -1,5 +1,5 @@
 """Thin Python binding of the C ABI in ``include/dropcompute.h`` (and of the measurement and tuning aids in
-``include/dropcompute_dev.h``).
+``include/dropcompute_dev.h`` and the training operators in ``include/dropcompute_train.h``).
 
 Argument marshalling only: every function checks dtype/device/contiguity of the torch tensors it is
 given, passes their device pointers and the current CUDA stream to the library entry point of the
@@ -30,6 +30,10 @@ EXPORTS = (
     "dc_argmax_tau", "dc_sweep_device",
     "dc_closed_form", "dc_sweep_host_workspace_bytes", "dc_sweep_host", "dc_check_inputs", "dc_device_status",
     "dc_status_string",
+)
+TRAIN_EXPORTS = (
+    "dc_embed", "dc_embed_backward_workspace_bytes", "dc_embed_backward", "dc_gelu_save8", "dc_gelu_save8_backward",
+    "dc_vocab_loss_workspace_bytes", "dc_vocab_loss", "dc_vocab_loss_backward", "dc_train_status",
 )
 DEV_EXPORTS = ("dc_simulate_plan", "dc_tune", "dc_launch_count", "dc_read_probe", "dc_kernel_version")
 
@@ -81,6 +85,18 @@ _lib.dc_status_string.restype = ctypes.c_char_p
 _lib.dc_kernel_version.argtypes = []
 _lib.dc_kernel_version.restype = ctypes.c_char_p
 _lib.dc_launch_count.argtypes = [_i32, _i64, _i64, _i64, _i32, _i64]
+_lib.dc_embed.argtypes = [_p, _i64, _i32, _p, _i64, _i64, _i64, _f32, _i64, _p, _i64, _p]
+_lib.dc_embed_backward_workspace_bytes.argtypes = [_i64, _i64, _i64]
+_lib.dc_embed_backward.argtypes = [_p, _i64, _i32, _p, _i64, _i64, _i64, _f32, _i64, _p, _i64, _i32, _i32, _p, _sz, _p]
+_lib.dc_gelu_save8.argtypes = [_p, _i64, _i32, _i64, _i64, _p, _i64, _p, _p, _p]
+_lib.dc_gelu_save8_backward.argtypes = [_p, _i64, _i32, _p, _p, _i64, _i64, _p, _i64, _p, _i64, _p]
+_lib.dc_vocab_loss_workspace_bytes.argtypes = [_i64, _i64, _i64, _p, _i64, _i32]
+_lib.dc_vocab_loss.argtypes = [_p, _i64, _p, _i64, _i32, _p, _i64, _i64, _i64, _i64, _f32, _p, _p, _p, _sz, _p]
+_lib.dc_vocab_loss_backward.argtypes = [_p, _i64, _p, _i64, _i32, _p, _i64, _i64, _i64, _i64, _f32, _p, _p, _p, _i64, _p, _i64, _i32,
+                                        _i32, _p, _sz, _p]
+_lib.dc_train_status.argtypes = [_p]
+for _name in TRAIN_EXPORTS:
+    getattr(_lib, _name).restype = _sz if _name.endswith("_bytes") else ctypes.c_int
 for _name in ("dc_simulate", "dc_simulate_ex", "dc_reduce_trials", "dc_argmax_tau", "dc_sweep_host", "dc_check_inputs",
               "dc_device_status", "dc_simulate_plan", "dc_launch_count", "dc_sweep_device", "dc_read_probe"):
     getattr(_lib, _name).restype = ctypes.c_int
@@ -389,3 +405,223 @@ def sweep(latencies: torch.Tensor, taus: torch.Tensor, t_comm: float, rule: int 
     dc_reduce_trials(out_step, out_done, out_sync, N, M, stats, baseline, ws)
     dc_argmax_tau(stats, taus, objective, out_k=k_star, out_tau=tau_star, out_value=value)
     return SweepResult(out_step, out_done, out_sync, stats, baseline, k_star, tau_star, value)
+
+
+# --- training operators (include/dropcompute_train.h) --------------------------------------------------------------
+# Matrices are [..., D] with adjacent elements in a row and evenly spaced rows; leading dimensions are flattened.
+
+_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+SAVE8_GROUP = 128
+EMBED_MAX_V = 4194304
+
+
+def _matrix(t: torch.Tensor, name: str, device: Optional[torch.device] = None, dtype: Optional[torch.dtype] = None):
+    """(pointer, row stride, rows, columns) of a tensor seen as a matrix."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype not in _DTYPE or (dtype is not None and t.dtype != dtype):
+        raise TypeError(f"{name} must be {dtype or 'bfloat16, float16 or float32'}, got {t.dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
+    if t.dim() < 1:
+        raise ValueError(f"{name} must have at least one dimension")
+    m = t if t.dim() == 2 else t.view(-1, t.shape[-1]) if t.numel() else t.reshape(0, t.shape[-1])
+    rows, cols = m.shape
+    if cols > 1 and rows > 0 and m.stride(1) != 1:
+        raise ValueError(f"the elements of a row of {name} must be adjacent")
+    return m.data_ptr(), (m.stride(0) if rows > 1 else max(1, cols)), rows, cols
+
+
+def _vector(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, device: torch.device) -> int:
+    p = _dev(t, dtype, name)
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold {n} values, got {t.numel()}")
+    return p
+
+
+def _same(name: str, got, want) -> None:
+    if tuple(got) != tuple(want):
+        raise ValueError(f"{name} must be {tuple(want)}, got {tuple(got)}")
+
+
+def _call(device: torch.device, where: str, fn, *args) -> None:
+    """Calls `fn(*args, stream)` with `device` current."""
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream), where)
+        return
+    with torch.cuda.device(device):
+        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream), where)
+
+
+def _workspace(ws: Optional[torch.Tensor], need: int, device: torch.device) -> torch.Tensor:
+    return torch.empty(need, dtype=torch.uint8, device=device) if ws is None else ws
+
+
+def dc_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, pad_id: int = -1) -> None:
+    """``dc_embed``: out[n] = scale * table[ids[n]]; zeros where ids[n] == pad_id, NaN where ids[n] is outside the table."""
+    t, ts, V, D = _matrix(table, "table")
+    o, os_, N, Do = _matrix(out, "out", table.device, table.dtype)
+    _same("out", (N, Do), (ids.numel(), D))
+    _call(table.device, "dc_embed", _lib.dc_embed, t, ts, _DTYPE[table.dtype], _vector(ids, "ids", torch.int64, N, table.device), N, V, D,
+          scale, pad_id, o, os_)
+
+
+def dc_embed_backward_workspace_bytes(N: int, V: int, D: int) -> int:
+    return int(_lib.dc_embed_backward_workspace_bytes(N, V, D))
+
+
+def dc_embed_backward(dout: torch.Tensor, ids: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
+                      pad_id: int = -1, accumulate: bool = False) -> None:
+    """``dc_embed_backward``: dtable[v] (+)= scale * sum of dout[n] over the places n of token v; dtable of dout's type or fp32."""
+    d, ds, N, D = _matrix(dout, "dout")
+    t, ts, V, Dt = _matrix(dtable, "dtable", dout.device)
+    _same("dtable", (V, Dt), (V, D))
+    _call(dout.device, "dc_embed_backward", _lib.dc_embed_backward, d, ds, _DTYPE[dout.dtype], _vector(ids, "ids", torch.int64, N, dout.device),
+          N, V, D, scale, pad_id, t, ts, _DTYPE[dtable.dtype], int(accumulate), _dev(workspace, torch.uint8, "workspace"), workspace.numel())
+
+
+def dc_gelu_save8(x: torch.Tensor, y: torch.Tensor, q: torch.Tensor, scales: torch.Tensor) -> None:
+    """``dc_gelu_save8``: y = gelu(x), q and scales = x in 8 bits (q int8 of x's shape, scales [rows, ceil(D / 128)] fp32)."""
+    p, xs, N, D = _matrix(x, "x")
+    o, ys, *shape = _matrix(y, "y", x.device, x.dtype)
+    _same("y", shape, (N, D))
+    _call(x.device, "dc_gelu_save8", _lib.dc_gelu_save8, p, xs, _DTYPE[x.dtype], N, D, o, ys, _vector(q, "q", torch.int8, N * D, x.device),
+          _vector(scales, "scales", torch.float32, N * -(-D // SAVE8_GROUP), x.device))
+
+
+def dc_gelu_save8_backward(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, dx: torch.Tensor,
+                           y_again: Optional[torch.Tensor] = None) -> None:
+    """``dc_gelu_save8_backward``: dx = dy * gelu'(x^) with x^ read back from 8 bits, and y_again = gelu(x^) where it is given."""
+    p, ds, N, D = _matrix(dy, "dy")
+    o, xs, *shape = _matrix(dx, "dx", dy.device, dy.dtype)
+    _same("dx", shape, (N, D))
+    r, rs = None, 0
+    if y_again is not None:
+        r, rs, *shape = _matrix(y_again, "y_again", dy.device, dy.dtype)
+        _same("y_again", shape, (N, D))
+    _call(dy.device, "dc_gelu_save8_backward", _lib.dc_gelu_save8_backward, p, ds, _DTYPE[dy.dtype], _vector(q, "q", torch.int8, N * D, dy.device),
+          _vector(scales, "scales", torch.float32, N * -(-D // SAVE8_GROUP), dy.device), N, D, o, xs, r, rs)
+
+
+def dc_vocab_loss_workspace_bytes(N: int, weight: torch.Tensor, backward: bool) -> int:
+    w, ws, V, D = _matrix(weight, "weight")
+    return int(_lib.dc_vocab_loss_workspace_bytes(N, V, D, w, ws, int(backward)))
+
+
+def dc_vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                  workspace: torch.Tensor, ignore_index: int = -100, logit_scale: float = 1.0) -> None:
+    """``dc_vocab_loss``: loss[n] = log sum_v exp l[n][v] - l[n][targets[n]], l = logit_scale * hidden @ weight.T; 0 where
+    targets[n] == ignore_index.  loss, lse fp32."""
+    h, hs, N, D = _matrix(hidden, "hidden")
+    w, ws, V, Dw = _matrix(weight, "weight", hidden.device, hidden.dtype)
+    _same("weight", (V, Dw), (V, D))
+    _call(hidden.device, "dc_vocab_loss", _lib.dc_vocab_loss, h, hs, w, ws, _DTYPE[hidden.dtype],
+          _vector(targets, "targets", torch.int64, N, hidden.device), N, V, D, ignore_index, logit_scale,
+          _vector(loss, "loss", torch.float32, N, hidden.device), _vector(lse, "lse", torch.float32, N, hidden.device),
+          _dev(workspace, torch.uint8, "workspace"), workspace.numel())
+
+
+def dc_vocab_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                           dhidden: Optional[torch.Tensor], dweight: Optional[torch.Tensor], workspace: torch.Tensor,
+                           ignore_index: int = -100, logit_scale: float = 1.0, accumulate: bool = False) -> None:
+    """``dc_vocab_loss_backward``: the gradients of dc_vocab_loss; either may be None; dweight of the weight's type or fp32."""
+    h, hs, N, D = _matrix(hidden, "hidden")
+    w, ws, V, Dw = _matrix(weight, "weight", hidden.device, hidden.dtype)
+    _same("weight", (V, Dw), (V, D))
+    dh, dhs, dw, dws, dwt = None, 0, None, 0, hidden.dtype
+    if dhidden is not None:
+        dh, dhs, *shape = _matrix(dhidden, "dhidden", hidden.device, hidden.dtype)
+        _same("dhidden", shape, (N, D))
+    if dweight is not None:
+        dw, dws, *shape = _matrix(dweight, "dweight", hidden.device)
+        _same("dweight", shape, (V, D))
+        dwt = dweight.dtype
+    _call(hidden.device, "dc_vocab_loss_backward", _lib.dc_vocab_loss_backward, h, hs, w, ws, _DTYPE[hidden.dtype],
+          _vector(targets, "targets", torch.int64, N, hidden.device), N, V, D, ignore_index, logit_scale,
+          _vector(lse, "lse", torch.float32, N, hidden.device), _vector(dloss, "dloss", torch.float32, N, hidden.device),
+          dh, dhs, dw, dws, _DTYPE[dwt], int(accumulate), _dev(workspace, torch.uint8, "workspace"), workspace.numel())
+
+
+def dc_train_status() -> int:
+    """Reads and clears the training kernels' expired-wait mask of the current device; raises if any wait expired."""
+    flags = ctypes.c_uint32(0)
+    _check(_lib.dc_train_status(ctypes.byref(flags)), f"dc_train_status (flags {flags.value:#x})")
+    return int(flags.value)
+
+
+# The same with outputs and workspaces allocated by torch.
+
+def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, pad_id: int = -1) -> torch.Tensor:
+    out = torch.empty((*ids.shape, table.shape[-1]), dtype=table.dtype, device=table.device)
+    dc_embed(table, ids, out, scale, pad_id)
+    return out
+
+
+def embed_backward(dout: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0, pad_id: int = -1,
+                   dtable: Optional[torch.Tensor] = None, accumulate: bool = False, dtype: Optional[torch.dtype] = None,
+                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The table's gradient [V, D]: a new tensor of `dtype` (dout's by default), or `dtable` written or added to."""
+    D = dout.shape[-1]
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate needs the dtable to add to")
+        dtable = torch.empty((V, D), dtype=dtype or dout.dtype, device=dout.device)
+    else:
+        _same("dtable", dtable.shape, (V, D))
+    dc_embed_backward(dout, ids, dtable, _workspace(workspace, dc_embed_backward_workspace_bytes(ids.numel(), V, D), dout.device), scale,
+                      pad_id, accumulate)
+    return dtable
+
+
+class Saved8(NamedTuple):
+    y: torch.Tensor        # gelu(x), x's type and shape
+    q: torch.Tensor        # int8, x's shape
+    scales: torch.Tensor   # fp32 [..., ceil(D / 128)]
+
+
+def gelu_save8(x: torch.Tensor) -> Saved8:
+    D = x.shape[-1]
+    r = Saved8(torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(x.shape, dtype=torch.int8, device=x.device),
+               torch.empty((*x.shape[:-1], -(-D // SAVE8_GROUP)), dtype=torch.float32, device=x.device))
+    dc_gelu_save8(x, *r)
+    return r
+
+
+def gelu_save8_backward(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, want_y: bool = False):
+    """dx, or (dx, y_again) with want_y."""
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+    y = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device) if want_y else None
+    dc_gelu_save8_backward(dy, q, scales, dx, y)
+    return (dx, y) if want_y else dx
+
+
+class VocabLoss(NamedTuple):
+    loss: torch.Tensor   # fp32, targets' shape
+    lse: torch.Tensor    # fp32, targets' shape; what the backward pass needs
+
+
+def vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100, logit_scale: float = 1.0,
+               workspace: Optional[torch.Tensor] = None) -> VocabLoss:
+    loss = torch.empty(targets.shape, dtype=torch.float32, device=hidden.device)
+    lse = torch.empty(targets.shape, dtype=torch.float32, device=hidden.device)
+    dc_vocab_loss(hidden, weight, targets, loss, lse,
+                  _workspace(workspace, dc_vocab_loss_workspace_bytes(targets.numel(), weight, False), hidden.device), ignore_index, logit_scale)
+    return VocabLoss(loss, lse)
+
+
+def vocab_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                        ignore_index: int = -100, logit_scale: float = 1.0, dweight: Optional[torch.Tensor] = None,
+                        accumulate: bool = False, want_dhidden: bool = True, want_dweight: bool = True,
+                        workspace: Optional[torch.Tensor] = None):
+    """(dhidden, dweight): dweight is a new tensor of the weight's type, or the given one (that type or fp32) written or added to."""
+    if accumulate and dweight is None:
+        raise ValueError("accumulate needs the dweight to add to")
+    dh = torch.empty(hidden.shape, dtype=hidden.dtype, device=hidden.device) if want_dhidden else None
+    if dweight is None and want_dweight:
+        dweight = torch.empty(weight.shape, dtype=weight.dtype, device=weight.device)
+    dc_vocab_loss_backward(hidden, weight, targets, lse, dloss, dh, dweight,
+                           _workspace(workspace, dc_vocab_loss_workspace_bytes(targets.numel(), weight, True), hidden.device),
+                           ignore_index, logit_scale, accumulate)
+    return dh, dweight

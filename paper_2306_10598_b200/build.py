@@ -1,22 +1,28 @@
-"""Builds libdropcompute.so (the C-ABI library) in-tree with nvcc for sm_100a."""
+"""Builds libdropcompute.so (the C-ABI library) in-tree with nvcc for sm_100a.
+
+One object per translation unit -- the sweep (csrc/dropcompute.cu) and each training operator (csrc/train/*.cu) -- compiled
+side by side and linked into one library.  Objects are kept in _build/ under a hash of what they were made from, so a change
+to one operator does not compile the sweep again."""
 from __future__ import annotations
 
 import hashlib
 import os
 import shutil
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "dropcompute.cu")
-HDRS = (os.path.join(ROOT, "include", "dropcompute.h"), os.path.join(ROOT, "include", "dropcompute_dev.h"))
+TRAIN = os.path.join(PKG, "csrc", "train")
+INCLUDE = os.path.join(ROOT, "include")
+HDRS = tuple(os.path.join(INCLUDE, h) for h in ("dropcompute.h", "dropcompute_dev.h", "dropcompute_train.h"))
 LIB = os.path.join(PKG, "libdropcompute.so")
+OBJECTS = os.path.join(PKG, "_build")
 
-NVCC_FLAGS = [
-    "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "--fmad=false",           # every fp32 operation of the sweep is a single IEEE operation, never contracted
-    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
-]
+COMMON_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
+SWEEP_FLAGS = ["--fmad=false"]   # every fp32 operation of the sweep is a single IEEE operation, never contracted
+LINK_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-cudart", "static"]
 
 
 def _nvcc() -> str:
@@ -31,8 +37,12 @@ def _cuda_sources():
     return sorted(os.path.join(csrc, f) for f in os.listdir(csrc) if f.endswith((".cu", ".cuh")))
 
 
+def _train_sources():
+    return sorted(os.path.join(TRAIN, f) for f in os.listdir(TRAIN) if f.endswith((".cu", ".cuh")))
+
+
 def source_hash() -> str:
-    """Hash of the CUDA sources (names and contents), baked into the library as dc_kernel_version(): a profile
+    """Hash of the sweep's CUDA sources (names and contents), baked into the library as dc_kernel_version(): a profile
     filed under one hash is never reported for a library built from other kernels."""
     h = hashlib.sha1()
     for path in _cuda_sources():
@@ -46,24 +56,54 @@ def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(f) > t for f in (*_cuda_sources(), *HDRS, os.path.abspath(__file__)))
+    return any(os.path.getmtime(f) > t for f in (*_cuda_sources(), *_train_sources(), *HDRS, os.path.abspath(__file__)))
+
+
+def _units():
+    """(source, flags, what it is made from) of every translation unit."""
+    sweep = [*SWEEP_FLAGS, f'-DDC_SOURCE_HASH="{source_hash()}"', "-I", os.path.dirname(SRC)]
+    yield SRC, sweep, (*_cuda_sources(), *HDRS[:2])
+    shared = [f for f in _train_sources() if f.endswith(".cuh")]
+    for f in _train_sources():
+        if f.endswith(".cu"):
+            yield f, ["-I", TRAIN], (f, *shared, HDRS[0], HDRS[2])
+
+
+def _compile(src: str, flags: list, made_from: tuple, force: bool, verbose: bool):
+    cmd = [_nvcc(), *COMMON_FLAGS, *flags, "-I", INCLUDE]
+    h = hashlib.sha1(" ".join(a.replace(ROOT, "") for a in cmd).encode())
+    for path in made_from:
+        with open(path, "rb") as f:
+            h.update(f.read())
+    name = os.path.splitext(os.path.basename(src))[0]
+    obj = os.path.join(OBJECTS, f"{name}-{h.hexdigest()[:16]}.o")
+    if os.path.exists(obj) and not force and not verbose:
+        return obj, ""
+    tmp = obj + f".tmp{os.getpid()}"
+    res = subprocess.run([*cmd, *(["-Xptxas", "-v"] if verbose else []), "-c", "-o", tmp, src], capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"nvcc failed on {src}:\n" + res.stdout + res.stderr)
+    for old in os.listdir(OBJECTS):
+        if old.startswith(name + "-") and old.endswith(".o") and os.path.join(OBJECTS, old) != obj:
+            os.unlink(os.path.join(OBJECTS, old))
+    os.replace(tmp, obj)
+    return obj, res.stdout + res.stderr
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
+    os.makedirs(OBJECTS, exist_ok=True)
+    units = list(_units())
+    with ThreadPoolExecutor(max_workers=max(1, min(len(units), os.cpu_count() or 1))) as pool:
+        done = list(pool.map(lambda u: _compile(*u, force, verbose), units))
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [_nvcc(), *NVCC_FLAGS, f'-DDC_SOURCE_HASH="{source_hash()}"', "-I", os.path.join(ROOT, "include"),
-           "-I", os.path.dirname(SRC), "-o", tmp, SRC]
-    if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    res = subprocess.run([_nvcc(), *LINK_FLAGS, "-o", tmp, *(obj for obj, _ in done)], capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        raise RuntimeError("nvcc failed to link:\n" + res.stdout + res.stderr)
     os.replace(tmp, LIB)
     if verbose:
-        print(res.stdout + res.stderr)
+        print("".join(said for _, said in done))
     return LIB
 
 

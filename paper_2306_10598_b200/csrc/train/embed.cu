@@ -1,0 +1,355 @@
+// dc_embed and dc_embed_backward: embedding lookup with scaling, and its gradient summed by token.
+//
+// The gradient of a token is the sum over every place where it occurs; tokens of text fall like 1 / rank, so one token
+// can hold several per cent of all places.  Places are grouped by token first (embed_sort), and the sum then runs over
+// equal tiles of the grouped list, whatever the tokens are: a token that is spread over several tiles leaves one partial
+// sum per tile, which embed_join adds in order.  No floating-point atomics, so two calls give the same bits.
+#include "train_common.cuh"
+
+namespace dct {
+
+constexpr int kTile = 32;            // places of the grouped list per tile
+constexpr int kBuckets = 128;        // blocks of embed_sort; more where a bucket would hold more than kMaxKeys tokens
+constexpr int kMaxKeys = 4096;
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kList = 2048;          // places of a bucket that are put in order at a time
+
+// ---- lookup: a warp takes (row, chunk of columns), four packs to a lane ------------------------------------------------
+
+template <class T, int V>
+__global__ void __launch_bounds__(256) embed_kernel(const T *__restrict__ table, int64_t ts, const int64_t *__restrict__ ids, int64_t N, int64_t vocab,
+                                                    int64_t D, float scale, int64_t pad, T *__restrict__ out, int64_t os, int32_t chunks)
+{
+    constexpr int U = 4;
+    const int lane = threadIdx.x & 31;
+    const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t n = task / chunks;
+    if (n >= N) return;
+    const int64_t c0 = (task - n * chunks) * (U * 32 * V) + lane * V;
+    const int64_t id = ids[n];
+    T *o = out + n * os;
+    if (id == pad || id < 0 || id >= vocab) {
+        Pack<T, V> fill;
+#pragma unroll
+        for (int i = 0; i < V; ++i) fill.v[i] = from_f<T>(id == pad ? 0.0f : __uint_as_float(0x7fffffffu));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (c0 + u * 32 * V < D) *reinterpret_cast<Pack<T, V> *>(o + c0 + u * 32 * V) = fill;
+        return;
+    }
+    const T *r = table + id * ts;
+    Pack<T, V> p[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (c0 + u * 32 * V < D) p[u] = *reinterpret_cast<const Pack<T, V> *>(r + c0 + u * 32 * V);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (c0 + u * 32 * V >= D) break;
+#pragma unroll
+        for (int i = 0; i < V; ++i) p[u].v[i] = from_f<T>(to_f(p[u].v[i]) * scale);
+        *reinterpret_cast<Pack<T, V> *>(o + c0 + u * 32 * V) = p[u];
+    }
+}
+
+// ---- grouping the places by token ----------------------------------------------------------------------------------------
+
+// Block b collects the places of tokens with token mod buckets = b, in order of place, and writes them token by token.
+// Every block reads all ids (from L2), so it also counts what goes before its own part: no block waits for another.
+__global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__restrict__ ids, int32_t N, int64_t vocab, int64_t pad, int32_t log_buckets,
+                                                           int32_t *__restrict__ place, int32_t *__restrict__ token, int32_t *__restrict__ live)
+{
+    extern __shared__ int32_t hist[];                      // [keys]: how often each token of the bucket occurs, then where it goes
+    __shared__ int32_t list_place[kList], list_key[kList];
+    __shared__ int32_t warp_mine[kSortWarps], warp_less[kSortWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t bucket = blockIdx.x, mask = gridDim.x - 1;
+    const int32_t keys = (int32_t)((vocab + mask) >> log_buckets);
+    for (int32_t k = tid; k < keys; k += kSortThreads) hist[k] = 0;
+    __syncthreads();
+
+    const int32_t seg = (N + kSortThreads - 1) / kSortThreads * 32;              // places of a warp, in order
+    const int64_t lo = (int64_t)warp * seg, hi = lo + seg < N ? lo + seg : N;
+    int32_t mine = 0, less = 0;
+    for (int64_t i = lo + lane; i < hi; i += 32) {
+        const int64_t id = ids[i];
+        const bool ok = id >= 0 && id < vocab && id != pad;
+        const int32_t b = (int32_t)id & mask;
+        if (ok && b == bucket) { ++mine; atomicAdd(&hist[id >> log_buckets], 1); }
+        less += ok && b < bucket;
+    }
+    mine = __reduce_add_sync(~0u, mine);
+    less = __reduce_add_sync(~0u, less);
+    if (lane == 0) { warp_mine[warp] = mine; warp_less[warp] = less; }
+    __syncthreads();
+    int32_t begin = 0, total = 0, first = 0;                                      // of this warp, of the bucket, of the bucket's part
+    for (int w = 0; w < kSortWarps; ++w) {
+        if (w == warp) begin = total;
+        total += warp_mine[w];
+        first += warp_less[w];
+    }
+    if (bucket == mask && tid == 0) *live = first + total;
+
+    // exclusive sum over the tokens of the bucket: each thread a run of neighbours, then the warps' totals
+    __shared__ int32_t warp_sum[kSortWarps];
+    const int32_t run = (keys + kSortThreads - 1) / kSortThreads, k0 = tid * run, k1 = min(keys, k0 + run);
+    int32_t own = 0;
+    for (int32_t k = k0; k < k1; ++k) own += hist[k];
+    int32_t upto = own;
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t o = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 31) warp_sum[warp] = upto;
+    __syncthreads();
+    int32_t at = upto - own;
+    for (int w = 0; w < warp; ++w) at += warp_sum[w];
+    for (int32_t k = k0; k < k1; ++k) { const int32_t c = hist[k]; hist[k] = at; at += c; }
+
+    for (int32_t from = 0; from < total; from += kList) {
+        __syncthreads();
+        int32_t r = begin;
+        if (begin < from + kList && begin + mine > from)
+            for (int64_t i0 = lo; i0 < hi; i0 += 32) {
+                const int64_t i = i0 + lane;
+                const int64_t id = i < hi ? ids[i] : -1;
+                const bool is = id >= 0 && id < vocab && id != pad && ((int32_t)id & mask) == bucket;
+                const uint32_t all = __ballot_sync(~0u, is);
+                const int32_t s = r + __popc(all & ((1u << lane) - 1)) - from;
+                if (is && s >= 0 && s < kList) { list_place[s] = (int32_t)i; list_key[s] = (int32_t)(id >> log_buckets); }
+                r += __popc(all);
+            }
+        __syncthreads();
+        if (warp == 0) {
+            const int32_t m = min(kList, total - from);
+            for (int32_t j0 = 0; j0 < m; j0 += 32) {
+                const int32_t j = j0 + lane;
+                const int32_t key = j < m ? list_key[j] : -1;
+                const uint32_t same = __match_any_sync(~0u, key);
+                const int32_t rank = __popc(same & ((1u << lane) - 1));
+                int32_t to = j < m ? hist[key] : 0;
+                __syncwarp();
+                if (j < m) {
+                    if (rank == 0) hist[key] = to + __popc(same);
+                    to += first + rank;
+                    place[to] = list_place[j];
+                    token[to] = (key << log_buckets) + bucket;
+                }
+                __syncwarp();
+            }
+        }
+    }
+}
+
+// ---- sums over the grouped list -------------------------------------------------------------------------------------------
+
+template <class O, int V> __device__ __forceinline__ void finish_row(O *row, const float (&sum)[V], float scale, bool accumulate)
+{
+    Pack<O, V> o;
+    if (accumulate) o = *reinterpret_cast<const Pack<O, V> *>(row);
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.v[i] = from_f<O>(accumulate ? to_f(o.v[i]) + scale * sum[i] : scale * sum[i]);
+    *reinterpret_cast<Pack<O, V> *>(row) = o;
+}
+
+// A warp takes (tile, 32 V columns).  part[tile][0] is the sum of the places at the tile's start whose token began in an
+// earlier tile, part[tile][1] of those at its end whose token goes on in the next one.
+template <class T, class O, int V>
+__global__ void __launch_bounds__(128) embed_sum(const T *__restrict__ dout, int64_t ds, const int32_t *__restrict__ place, const int32_t *__restrict__ token,
+                                                 const int32_t *__restrict__ live, int64_t D, float scale, O *__restrict__ dtable, int64_t ts, bool accumulate,
+                                                 float *__restrict__ part, int64_t pitch, int32_t chunks)
+{
+    constexpr int U = 8;                                   // rows on their way at a time
+    const int lane = threadIdx.x & 31;
+    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int64_t tile = task / chunks;
+    const int64_t c = (task - tile * chunks) * (32 * V) + lane * V;
+    const int32_t n = *live;
+    const int64_t begin = tile * kTile;
+    if (begin >= n) return;
+    const int32_t m = (int32_t)min((int64_t)kTile, n - begin);
+    const int32_t my_place = lane < m ? place[begin + lane] : 0;
+    const int32_t my_token = lane < m ? token[begin + lane] : -1;
+    const int32_t before = begin > 0 ? token[begin - 1] : -1, after = begin + m < n ? token[begin + m] : -1;
+    float sum[V] = {};
+    int32_t run_from = 0;
+    for (int32_t j0 = 0; j0 < m; j0 += U) {
+        Pack<T, V> p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t at = __shfl_sync(~0u, my_place, (j0 + u) & 31);
+            if (j0 + u < m && c < D) p[u] = *reinterpret_cast<const Pack<T, V> *>(dout + (int64_t)at * ds + c);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t j = j0 + u;
+            if (j >= m) break;
+            const int32_t tok = __shfl_sync(~0u, my_token, j);
+            const int32_t next = j + 1 < m ? __shfl_sync(~0u, my_token, (j + 1) & 31) : after;
+            if (c < D) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] += to_f(p[u].v[i]);
+            }
+            const bool ends = next != tok, last = j + 1 == m;
+            if (ends || last) {
+                const bool began_earlier = run_from == 0 && before == tok;
+                if (c < D) {
+                    if (ends && !began_earlier) {
+                        finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
+                    } else {
+                        float *to = part + (tile * 2 + (began_earlier ? 0 : 1)) * pitch + c;
+#pragma unroll
+                        for (int i = 0; i < V; ++i) to[i] = sum[i];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+                run_from = j + 1;
+            }
+        }
+    }
+}
+
+// A token that begins in a tile and goes on in the next: its partial sums in the order of the tiles.
+template <class O, int V>
+__global__ void __launch_bounds__(128) embed_join(const int32_t *__restrict__ token, const int32_t *__restrict__ live, int64_t D, float scale,
+                                                  O *__restrict__ dtable, int64_t ts, bool accumulate, const float *__restrict__ part, int64_t pitch,
+                                                  int32_t chunks)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int64_t tile = task / chunks;
+    const int64_t c = (task - tile * chunks) * (32 * V) + lane * V;
+    const int32_t n = *live;
+    const int64_t end = (tile + 1) * kTile;
+    if (end >= n) return;                                                    // the last tile has nothing behind it
+    const int32_t tok = token[end - 1];
+    if (token[end] != tok) return;                                           // nothing goes on
+    if (tile > 0 && token[tile * kTile] == tok && token[tile * kTile - 1] == tok) return;   // it began in an earlier tile
+    if (c >= D) return;
+    float sum[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] = part[(tile * 2 + 1) * pitch + c + i];
+    for (int64_t t = tile + 1; t * kTile < n && token[t * kTile] == tok; ++t)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] += part[t * 2 * pitch + c + i];
+    finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
+}
+
+struct SortPlan { int32_t log_buckets; int32_t keys; };
+inline SortPlan sort_plan(int64_t V)
+{
+    SortPlan p{7, 0};
+    static_assert(kBuckets == 1 << 7, "log_buckets starts at kBuckets");
+    while (ceil_div(V, int64_t(1) << p.log_buckets) > kMaxKeys) ++p.log_buckets;
+    p.keys = (int32_t)ceil_div(V, int64_t(1) << p.log_buckets);
+    return p;
+}
+
+struct Work { int32_t *live, *place, *token; float *part; int64_t pitch; size_t bytes; };
+inline Work carve(void *base, int64_t N, int64_t D)
+{
+    Work w{};
+    char *p = (char *)base;
+    size_t at = 256;
+    w.live = (int32_t *)p;
+    w.place = (int32_t *)(p + at);
+    at += align_up((size_t)N * 4, 256);
+    w.token = (int32_t *)(p + at);
+    at += align_up((size_t)N * 4, 256);
+    w.part = (float *)(p + at);
+    w.pitch = ceil_div(D, 8) * 8;
+    at += align_up((size_t)ceil_div(N, kTile) * 2 * (size_t)w.pitch * 4, 256);
+    w.bytes = at;
+    return w;
+}
+
+template <class T, class O, int V>
+int backward_launch(const void *dout, int64_t ds, int64_t N, int64_t D, float scale, void *dtable, int64_t ts, bool accumulate, const Work &w, cudaStream_t st)
+{
+    const int32_t chunks = (int32_t)ceil_div(D, 32 * V);
+    const int64_t blocks = ceil_div(ceil_div(N, kTile) * chunks, 4);
+    if (blocks > INT32_MAX) return DC_ERR_RANGE;
+    embed_sum<T, O, V><<<(unsigned)blocks, 128, 0, st>>>((const T *)dout, ds, w.place, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch, chunks);
+    embed_join<O, V><<<(unsigned)blocks, 128, 0, st>>>(w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch, chunks);
+    return launched();
+}
+
+template <class T, int V>
+int lookup(const void *table, int64_t ts, const int64_t *ids, int64_t N, int64_t vocab, int64_t D, float scale, int64_t pad, void *out, int64_t os, cudaStream_t st)
+{
+    const int32_t chunks = (int32_t)ceil_div(D, 4 * 32 * V);
+    const int64_t blocks = ceil_div(N * chunks, 8);
+    if (blocks > INT32_MAX) return DC_ERR_RANGE;
+    embed_kernel<T, V><<<(unsigned)blocks, 256, 0, st>>>((const T *)table, ts, ids, N, vocab, D, scale, pad, (T *)out, os, chunks);
+    return launched();
+}
+
+inline int check(int64_t N, int64_t V, int64_t D, int32_t dtype)
+{
+    if (N < 0 || V <= 0 || D <= 0) return DC_ERR_SHAPE;
+    if (N > kMaxDim || V > kMaxDim || D > kMaxDim) return DC_ERR_RANGE;
+    if (dtype != DC_BF16 && dtype != DC_F16 && dtype != DC_F32) return DC_ERR_UNSUPPORTED;
+    return DC_OK;
+}
+
+}  // namespace dct
+
+using namespace dct;
+
+extern "C" int dc_embed(const void *table, int64_t table_stride, int32_t dtype, const int64_t *ids, int64_t N, int64_t V, int64_t D, float scale,
+                        int64_t pad_id, void *out, int64_t out_stride, void *stream)
+{
+    if (int e = check(N, V, D, dtype)) return e;
+    if (N == 0) return DC_OK;
+    if (!table || !ids || !out) return DC_ERR_NULL;
+    if (table_stride < D || out_stride < D) return DC_ERR_SHAPE;
+    const int eb = elem_bytes(dtype);
+    if (!on(table, eb) || !on(out, eb) || !on(ids, 8)) return DC_ERR_ALIGN;
+    if (pad_id < 0) pad_id = INT64_MIN;
+    const bool wide = D % (16 / eb) == 0 && rows_on(table, table_stride, eb, 16) && rows_on(out, out_stride, eb, 16);
+    const cudaStream_t st = (cudaStream_t)stream;
+#define DCT_LOOKUP(T, W) lookup<T, W>(table, table_stride, ids, N, V, D, scale, pad_id, out, out_stride, st)
+    if (dtype == DC_BF16) return wide ? DCT_LOOKUP(__nv_bfloat16, 8) : DCT_LOOKUP(__nv_bfloat16, 1);
+    if (dtype == DC_F16) return wide ? DCT_LOOKUP(__half, 8) : DCT_LOOKUP(__half, 1);
+    return wide ? DCT_LOOKUP(float, 4) : DCT_LOOKUP(float, 1);
+#undef DCT_LOOKUP
+}
+
+extern "C" size_t dc_embed_backward_workspace_bytes(int64_t N, int64_t V, int64_t D)
+{
+    if (N < 0 || V <= 0 || D <= 0 || N > kMaxDim || V > DC_EMBED_MAX_V || D > kMaxDim) return 0;
+    return carve(nullptr, N, D).bytes;
+}
+
+extern "C" int dc_embed_backward(const void *dout, int64_t dout_stride, int32_t dtype, const int64_t *ids, int64_t N, int64_t V, int64_t D, float scale,
+                                 int64_t pad_id, void *dtable, int64_t dtable_stride, int32_t dtable_dtype, int32_t accumulate, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    if (int e = check(N, V, D, dtype)) return e;
+    if (V > DC_EMBED_MAX_V) return DC_ERR_RANGE;
+    if (dtable_dtype != dtype && dtable_dtype != DC_F32) return DC_ERR_UNSUPPORTED;
+    if (!dtable || (N > 0 && (!dout || !ids))) return DC_ERR_NULL;
+    if (dtable_stride < D || (N > 0 && dout_stride < D)) return DC_ERR_SHAPE;
+    const int eb = elem_bytes(dtype), ob = elem_bytes(dtable_dtype);
+    if (!on(dtable, ob) || (N > 0 && (!on(dout, eb) || !on(ids, 8)))) return DC_ERR_ALIGN;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (N > 0 && (!workspace || !on(workspace, 256) || workspace_bytes < carve(nullptr, N, D).bytes)) return DC_ERR_WORKSPACE;
+    if (!accumulate && cudaMemset2DAsync(dtable, (size_t)dtable_stride * ob, 0, (size_t)D * ob, (size_t)V, st) != cudaSuccess) return DC_ERR_CUDA;
+    if (N == 0) return DC_OK;
+    const Work w = carve(workspace, N, D);
+    const SortPlan p = sort_plan(V);
+    if (pad_id < 0) pad_id = INT64_MIN;
+    embed_sort<<<1u << p.log_buckets, kSortThreads, (size_t)p.keys * 4, st>>>(ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token, w.live);
+    // packs of V elements on both sides: 16 bytes of dout, and as many elements of dtable
+    const int W = 16 / eb;
+    const bool wide = D % W == 0 && rows_on(dout, dout_stride, eb, 16) && rows_on(dtable, dtable_stride, ob, (size_t)(W * ob));
+#define DCT_SUM(T, O, V_) backward_launch<T, O, V_>(dout, dout_stride, N, D, scale, dtable, dtable_stride, accumulate != 0, w, st)
+    if (dtype == DC_F32) return wide ? DCT_SUM(float, float, 4) : DCT_SUM(float, float, 1);
+    if (dtype == DC_BF16) {
+        if (dtable_dtype == DC_F32) return wide ? DCT_SUM(__nv_bfloat16, float, 8) : DCT_SUM(__nv_bfloat16, float, 1);
+        return wide ? DCT_SUM(__nv_bfloat16, __nv_bfloat16, 8) : DCT_SUM(__nv_bfloat16, __nv_bfloat16, 1);
+    }
+    if (dtable_dtype == DC_F32) return wide ? DCT_SUM(__half, float, 8) : DCT_SUM(__half, float, 1);
+    return wide ? DCT_SUM(__half, __half, 8) : DCT_SUM(__half, __half, 1);
+#undef DCT_SUM
+}

@@ -1,0 +1,50 @@
+// What the training operators share: element types, vector loads and stores, reductions, host-side checks.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "dropcompute_train.h"
+
+namespace dct {
+
+constexpr int64_t kMaxDim = int64_t(1) << 30;
+
+// Bounds the launches of this library on one device; the multiprocessor count is read once per device.
+inline int sm_count()
+{
+    static int cached[64] = {};                 // 0 = not read yet; a racing second read stores the same value
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 0;
+    if (dev < 64) {
+        const int have = __atomic_load_n(&cached[dev], __ATOMIC_RELAXED);
+        if (have) return have;
+    }
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev < 64) __atomic_store_n(&cached[dev], n, __ATOMIC_RELAXED);
+    return n;
+}
+
+inline int launched() { return cudaGetLastError() == cudaSuccess ? DC_OK : DC_ERR_CUDA; }
+inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int elem_bytes(int32_t dtype) { return dtype == DC_F32 ? 4 : 2; }
+inline bool on(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// rows of a matrix whose starts all fall on `a`-byte boundaries
+inline bool rows_on(const void *p, int64_t stride, int eb, size_t a) { return on(p, a) && (size_t)(stride * eb) % a == 0; }
+
+// A pack of adjacent elements of a row: 16 bytes where rows start on 16-byte boundaries, one element otherwise.
+template <class T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
+
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <class T> __device__ __forceinline__ T from_f(float x);
+template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+}  // namespace dct
