@@ -1,190 +1,452 @@
-// The three products of the vocabulary loss, with what is done to a tile of them before it leaves the chip.
+// The products of the vocabulary loss on the tensor cores, with what is done to a tile before it leaves the chip.
+//
+// One persistent kernel serves all of them.  A pair of CTAs works on a tile of 256 x 256 results: each brings its 128 rows of
+// both operands (64 of the summed dimension at a time) into a ring in shared memory by bulk tensor copies, one thread of the
+// pair issues the products into tensor memory, and eight warps of each CTA take finished tiles from there.  Tensor memory
+// holds two tiles, so the products of one run while the other is taken out: exp, maxima and sums hide behind the products
+// (a tile is 2 * 256^2 * D flops = 8 D cycles of a pair, taking it out about 2000 cycles).
+//
+//   what    tile of                       rows x columns      summed over        leaves as
+//   kLoss   c h W^T                       tokens x vocab      hidden             (max, sum of exp) of each row and half tile
+//   kGrad   c h W^T of a piece            tokens x vocab      hidden             g in 16 bits
+//   kBack   dW = g^T h'  of the piece     vocab x hidden      tokens             dW, added to or not
+//           dh = g W     of the piece     tokens x hidden     a part of vocab    partial products in fp32
 #pragma once
 
-#include "train_common.cuh"
+#include "tensor_core.cuh"
 
 namespace dct {
 
-__device__ unsigned int g_train_wait_expired = 0;
-
 constexpr int kTileM = 256, kTileN = 256;   // rows and columns of a tile of the result
-constexpr int kRowBlock = 64;               // what a product over rows or tokens takes at a time
+constexpr int kRowBlock = 64;               // elements of the summed dimension to a stage of the ring
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // g of one piece of the vocabulary
+constexpr int kStages = 6, kStageBytes = 2 * 128 * 64 * 2;
+constexpr int kTcThreads = 384;             // warp 0 copies, warp 1 multiplies, warp 2 has the tensor memory, warps 4-11 take tiles out
+constexpr int kTcSmem = kStages * kStageBytes + 1024;
+constexpr int kMaxParts = 16;
+
+enum What { kLoss, kGrad, kBack };
 
 // What vocab_gather finds out on the device.
 struct Head {
-    int32_t rows;                           // labelled rows
-    float grad_scale, grad_unscale;         // power of two that g carries, and its inverse
+    int32_t rows;        // labelled rows
+    int32_t parts;       // parts of the vocabulary that dh is summed in
+    float top;           // the largest |dloss * logit_scale| among them, 1 where that is 0 or not finite
 };
 
-// Partial products of dh: one.
-__host__ __device__ inline int32_t split_of(int32_t rows, int32_t tiles_d, int32_t vocab_blocks) { return 1; }
-inline int64_t acc_rows(int64_t N, int32_t tiles_d) { return ceil_div(N, kTileM) * kTileM; }
-
-// ---- a plain tile product: 64 x 64 results, 256 threads with 4 x 4 each --------------------------------------------------
-
-constexpr int kS = 64, kK = 16;
-
-// C[i][j] = sum_k A(i,k) B(j,k); A(i,k) = a[i*ai + k*ak], zero outside [0,I) x [0,K); B alike.
-template <class T>
-__device__ __forceinline__ void tile_product(float (&c)[4][4], const T *a, int64_t ai, int64_t ak, int64_t i0, int64_t I, const T *b, int64_t bj, int64_t bk,
-                                             int64_t j0, int64_t J, int64_t K, float (*sa)[kS + 1], float (*sb)[kS + 1])
+// In how many parts of the vocabulary dh is summed: few tiles of dh leave most of the GPU idle, many parts cost fp32 traffic.
+// A pair of CTAs c takes units c, c + pairs, ...: first the tiles of dW (rb blocks each), then those of dh; the parts that give
+// the shortest longest list are taken.  Each unit is charged kUnitCost blocks for taking its tile out.  The tiles of dW count
+// whether dW is asked for or not, so that dh has the same bits either way.
+constexpr uint32_t kUnitCost = 6;
+__host__ __device__ inline uint32_t up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
+__host__ __device__ inline int32_t parts_of(uint32_t rows, uint32_t D, uint32_t vocab_blocks, uint32_t pairs, int64_t acc_rows)
 {
-    const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[i][j] = 0.0f;
-    for (int64_t k0 = 0; k0 < K; k0 += kK) {
-        __syncthreads();
-        for (int e = tid; e < kS * kK; e += 256) {
-            const int ia = ak == 1 ? e / kK : e % kS, ka = ak == 1 ? e % kK : e / kS;
-            sa[ka][ia] = i0 + ia < I && k0 + ka < K ? to_f(a[(i0 + ia) * ai + (k0 + ka) * ak]) : 0.0f;
-            const int ib = bk == 1 ? e / kK : e % kS, kb = bk == 1 ? e % kK : e / kS;
-            sb[kb][ib] = j0 + ib < J && k0 + kb < K ? to_f(b[(j0 + ib) * bj + (k0 + kb) * bk]) : 0.0f;
+    if (rows == 0) return 1;
+    const uint32_t td = up(D, kTileN), rb = up(rows, kRowBlock) + kUnitCost;
+    const uint32_t nw = up(vocab_blocks, kTileM / kRowBlock) * td, q = nw / pairs, r = nw % pairs;
+    uint32_t best = 1;
+    uint64_t least = ~0ull;
+    for (uint32_t s = 1; s <= kMaxParts && s <= vocab_blocks && (int64_t)s * rows <= acc_rows; ++s) {
+        const uint32_t len = up(vocab_blocks, s);
+        if (up(vocab_blocks, len) != s) continue;                       // the last part would be empty
+        const uint32_t cost = len + kUnitCost, n = up(rows, kTileM) * td * s, q2 = n / pairs, r2 = n % pairs, dw = r ? rb : 0, dh = r2 ? cost : 0;
+        const uint32_t extra = r + r2 > pairs ? dw + dh : dw > dh ? dw : dh;
+        const uint64_t total = (uint64_t)q * rb + (uint64_t)q2 * cost + extra;
+        if (total < least) { least = total; best = s; }
+    }
+    return (int32_t)best;
+}
+// rows of the fp32 partial products: every row once, and enough tiles for as many parts as fill the device
+inline int64_t acc_rows_for(int64_t N, int64_t D) { return ceil_div(N > 0 ? N : 1, kTileM) * kTileM + ceil_div(80, ceil_div(D, kTileN)) * kTileM; }
+
+struct Product {
+    const Head *head;
+    // kLoss, kGrad
+    const int32_t *label;
+    float scale;                    // logit_scale * log2(e): logits in powers of two
+    float2 *part; float *hit; int32_t part_pitch;
+    const float *lse;
+    void *grad; int32_t piece;
+    int32_t v0;                     // first of the piece
+    float grad_scale;               // power of two that g carries
+    // sizes: vocabulary (of the piece), hidden
+    int32_t V, D, Dp;
+    // kBack
+    void *dw; int64_t dw_stride; bool dw_f32, dw_add, dw_wide;
+    float *acc; bool first; int32_t vocab_blocks;   // vocab_blocks: of the first piece
+};
+
+struct Unit {
+    int32_t m, n, k, blocks, part;  // first row, column and block of the summed dimension; number of blocks
+    bool dw;
+};
+
+template <int WHAT> struct Units {
+    int32_t rows, count, tm, tn, nw, len, parts;
+    __device__ Units(const Product &p)
+    {
+        rows = p.head->rows;
+        tm = (rows + kTileM - 1) / kTileM;
+        if (WHAT == kBack) {
+            tn = (p.D + kTileN - 1) / kTileN;
+            nw = p.dw ? (p.V + kTileM - 1) / kTileM * tn : 0;
+            parts = p.head->parts;
+            len = (p.vocab_blocks + parts - 1) / parts;
+            count = nw + (p.acc ? tm * tn * parts : 0);
+        } else {
+            tn = (p.V + kTileN - 1) / kTileN;
+            count = tm * tn;
         }
-        __syncthreads();
+    }
+    __device__ __forceinline__ Unit get(int32_t u, const Product &p) const
+    {
+        Unit r;
+        r.k = r.part = 0;
+        r.dw = false;
+        if (WHAT != kBack) {
+            r.m = u % tm * kTileM;                          // all rows for one stretch of the vocabulary, so that W is read once
+            r.n = u / tm * kTileN;
+            r.blocks = p.Dp / kRowBlock;
+        } else if (u < nw) {
+            r.dw = true;
+            r.m = u / tn * kTileM;
+            r.n = u % tn * kTileN;
+            r.blocks = (rows + kRowBlock - 1) / kRowBlock;
+        } else {
+            u -= nw;
+            r.n = u % tn * kTileN;
+            u /= tn;
+            r.m = u % tm * kTileM;
+            r.part = u / tm;
+            r.k = r.part * len;
+            const int32_t have = (p.V + kRowBlock - 1) / kRowBlock;
+            r.blocks = max(0, min(len, have - r.k));
+        }
+        return r;
+    }
+};
+
+// ---- taking tiles out: a thread has one row, `col` is the first of 32 columns ------------------------------------------------
+
+__device__ __forceinline__ void store32(void *to, const uint32_t (&r)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]),
+                 "r"(r[7]) : "memory");
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)
+{
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __half)
+{
+    const __half2 x = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
+
+// Running maximum and sum of exp over 32 more logits (in powers of two).  Where nothing finite has been seen the maximum
+// stays -inf and the sum 0; a NaN reaches the sum, a +inf makes it NaN.
+__device__ __forceinline__ void online(const float (&v)[32], int32_t valid, float c, float &m, float &s)
+{
+    float z[32];
+    float t0 = m, t1 = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < kK; ++k) {
-            float x[4], y[4];
+    for (int i = 0; i < 32; i += 2) {
+        z[i] = i < valid ? v[i] * c : -INFINITY;
+        z[i + 1] = i + 1 < valid ? v[i + 1] * c : -INFINITY;
+        t0 = fmaxf(t0, z[i]);
+        t1 = fmaxf(t1, z[i + 1]);
+    }
+    const float top = fmaxf(t0, t1), ref = top == -INFINITY ? 0.0f : top;
+    float a = s * exp2_fast(m - ref), b = 0.0f;             // m = -inf: 0 times 0
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { x[i] = sa[k][ty * 4 + i]; y[i] = sb[k][tx * 4 + i]; }
+    for (int i = 0; i < 32; i += 2) {
+        a += exp2_fast(z[i] - ref);
+        b += exp2_fast(z[i + 1] - ref);
+    }
+    m = top;
+    s = a + b;
+}
+
+template <class T>
+__device__ __forceinline__ void put_weight_grad(const Product &p, int32_t row, int32_t col, const float (&v)[32], float unscale)
+{
+    if (row >= p.V || col >= p.D) return;
+    const int64_t at = (int64_t)row * p.dw_stride + col;
+    if (p.dw_wide && col + 32 <= p.D) {
+        if (p.dw_f32) {
+            float4 *o = reinterpret_cast<float4 *>((float *)p.dw + at);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 8; ++i) {
+                float4 x = make_float4(v[4 * i] * unscale, v[4 * i + 1] * unscale, v[4 * i + 2] * unscale, v[4 * i + 3] * unscale);
+                if (p.dw_add) { const float4 y = o[i]; x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w; }
+                o[i] = x;
+            }
+        } else {
+            Pack<T, 8> *o = reinterpret_cast<Pack<T, 8> *>((T *)p.dw + at);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) c[i][j] = fmaf(x[i], y[j], c[i][j]);
+            for (int i = 0; i < 4; ++i) {
+                Pack<T, 8> x;
+                if (p.dw_add) x = o[i];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x.v[j] = from_f<T>((p.dw_add ? to_f(x.v[j]) : 0.0f) + v[8 * i + j] * unscale);
+                o[i] = x;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        if (col + i >= p.D) break;
+        if (p.dw_f32) {
+            float *o = (float *)p.dw + at + i;
+            *o = (p.dw_add ? *o : 0.0f) + v[i] * unscale;
+        } else {
+            T *o = (T *)p.dw + at + i;
+            *o = from_f<T>((p.dw_add ? to_f(*o) : 0.0f) + v[i] * unscale);
         }
     }
 }
 
-#define DCT_SHARED __shared__ float sa[kK][kS + 1], sb[kK][kS + 1]; float c[4][4]; const int ty = threadIdx.x / 16, tx = threadIdx.x % 16
+// ---- the kernel ----------------------------------------------------------------------------------------------------------------
 
-template <class T>
-__global__ void __launch_bounds__(256) loss_kernel(const Head *head, const T *h, int64_t hs, const T *w, int64_t ws, const int32_t *label, int64_t V, int64_t D,
-                                                   float scale, float2 *part, float *hit, int32_t tiles_v)
+// a, b: operands of kLoss and kGrad, and of dh; a_dw, b_dw: of dW
+template <class T, int WHAT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
+vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUtensorMap b, const __grid_constant__ CUtensorMap a_dw,
+              const __grid_constant__ CUtensorMap b_dw, const __grid_constant__ Product p)
 {
-    DCT_SHARED;
-    const int64_t L = head->rows, i0 = (int64_t)blockIdx.y * kS, t = blockIdx.x;
-    if (i0 >= L) return;
-    float m[4], s[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { m[i] = -INFINITY; s[i] = 0.0f; }
-    for (int64_t j0 = t * kTileN; j0 < (t + 1) * kTileN && j0 < V; j0 += kS) {
-        tile_product(c, h, hs, 1, i0, L, w, ws, 1, j0, V, D, sa, sb);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t r = i0 + ty * 4 + i;
-            float top = m[i];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j0 + tx * 4 + j < V) {
-                    top = fmaxf(top, c[i][j] * scale);
-                    if (r < L && label[r] == j0 + tx * 4 + j) hit[r] = c[i][j] * scale;
+    constexpr bool kBf16 = sizeof(T) == 2 && !__is_same(T, __half);
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[kStages], empty[kStages], ready[2], taken[2];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up_at;
+    volatile int *gave_up = &gave_up_at;
+
+    const uint32_t ring = (smem_u32(raw) + 1023) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+    if (threadIdx.x == 0) {
+        tma_prefetch(&a);
+        tma_prefetch(&b);
+        if (WHAT == kBack) { tma_prefetch(&a_dw); tma_prefetch(&b_dw); }
+        gave_up_at = 0;
+        for (int i = 0; i < kStages; ++i) { bar_init(smem_u32(&full[i]), 1); bar_init(smem_u32(&empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(smem_u32(&ready[i]), 1); bar_init(smem_u32(&taken[i]), 16); }
+        bar_init_visible();
+    }
+    if (warp == 2) tmem_alloc(smem_u32(&tmem_at), 512);
+    tc_before_sync();
+    __syncthreads();
+    cluster_sync();
+    tc_after_sync();
+    const uint32_t tmem = tmem_at;
+    const Units<WHAT> units(p);
+
+    if (warp == 0 && lane == 0) {
+        uint32_t stage = 0, phase = 0;
+        for (int32_t u = pair; u < units.count && !*gave_up; u += pairs) {
+            const Unit t = units.get(u, p);
+            for (int32_t k = 0; k < t.blocks; ++k) {
+                if (!bar_wait(smem_u32(&empty[stage]), phase ^ 1, gave_up, 1u)) break;
+                const uint32_t bar = smem_u32(&full[stage]), to = ring + stage * kStageBytes, lead = in_cta(bar, 0);
+                if (rank == 0) bar_expect(bar, 2 * kStageBytes);
+                const int32_t at = (t.k + k) * kRowBlock, m = t.m + (int32_t)rank * 128, n = t.n + (int32_t)rank * 128;
+                if (WHAT != kBack) {
+                    tma_load(to, &a, at, m, lead);
+                    tma_load(to + 16384, &b, at, n, lead);
+                } else if (t.dw) {
+                    tma_load(to, &a_dw, m, at, lead);
+                    tma_load(to + 8192, &a_dw, m + 64, at, lead);
+                    tma_load(to + 16384, &b_dw, n, at, lead);
+                    tma_load(to + 24576, &b_dw, n + 64, at, lead);
+                } else {
+                    tma_load(to, &a, at, m, lead);
+                    tma_load(to + 16384, &b, n, at, lead);
+                    tma_load(to + 24576, &b, n + 64, at, lead);
                 }
-            float sum = m[i] == -INFINITY ? s[i] : s[i] * __expf(m[i] - top);
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+        }
+        // the products' last arrivals reach this CTA before it ends
+        for (int i = 0; i < kStages; ++i) {
+            if (!bar_wait(smem_u32(&empty[stage]), phase ^ 1, gave_up, 1u)) break;
+            if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+        for (int32_t u = pair; u < units.count && !*gave_up; u += pairs) {
+            const Unit t = units.get(u, p);
+            if (t.blocks == 0) continue;
+            if (!bar_wait(smem_u32(&taken[buf]), buf_phase ^ 1, gave_up, 2u)) break;
+            tc_after_sync();
+            const bool a_mn = WHAT == kBack && t.dw, b_mn = WHAT == kBack;
+            const uint32_t form = product_form<kBf16>(a_mn, b_mn);
+            // 16 of the summed dimension further: 32 bytes along a row (K-major), 16 rows (MN-major)
+            const uint32_t a_step = a_mn ? 2048 : 32, b_step = b_mn ? 2048 : 32;
+            for (int32_t k = 0; k < t.blocks; ++k) {
+                if (!bar_wait(smem_u32(&full[stage]), phase, gave_up, 4u)) break;
+                tc_after_sync();
+                const uint32_t at = ring + stage * kStageBytes;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j0 + tx * 4 + j < V) sum += top == -INFINITY && c[i][j] * scale == -INFINITY ? 0.0f : __expf(c[i][j] * scale - top);
-            m[i] = top;
-            s[i] = sum;
+                for (uint32_t i = 0; i < kRowBlock / 16; ++i)
+                    tc_product(tmem + buf * 256, operand(at + i * a_step, a_mn ? 8192 : 16), operand(at + 16384 + i * b_step, b_mn ? 8192 : 16), form, k + i > 0);
+                tc_commit(smem_u32(&empty[stage]));
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+            tc_commit(smem_u32(&ready[buf]));
+            buf ^= 1;
+            buf_phase ^= buf == 0;
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        uint32_t buf = 0, buf_phase = 0;
+        for (int32_t u = pair; u < units.count && !__any_sync(~0u, *gave_up); u += pairs) {
+            const Unit t = units.get(u, p);
+            const int32_t row = t.m + (int32_t)rank * 128 + quarter * 32 + lane;
+            const int32_t c0 = t.n + half * 128;
+            // what the row needs, on its way while the products run
+            int32_t label = -1;
+            float lse2 = 0.0f;
+            if (WHAT != kBack && row < units.rows) {
+                label = p.label[row];
+                if (WHAT == kGrad) { label -= p.v0; lse2 = p.lse[row] * 1.4426950408889634f; }
+            }
+            const float unscale = WHAT == kBack && t.dw ? p.head->top * p.grad_scale : 1.0f;
+            if (t.blocks > 0) {
+                if (!__all_sync(~0u, bar_wait(smem_u32(&ready[buf]), buf_phase, gave_up, 8u))) break;
+                tc_after_sync();
+            }
+            float m = -INFINITY, s = 0.0f, at_label = 0.0f;
+            const uint32_t from = tmem + buf * 256 + half * 128 + ((uint32_t)(quarter * 32) << 16);
+            __syncwarp();
+#pragma unroll 1
+            for (int j = 0; j < 4; ++j) {
+                const int32_t col = c0 + j * 32;
+                float v[32];
+                if (t.blocks > 0) {
+                    tmem_load(from + j * 32, v);
+                    tmem_load_done();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                }
+                if (WHAT == kLoss) {
+                    const int32_t valid = p.V - col;
+                    if (valid <= 0) break;
+                    if (valid >= 32) online(v, 32, p.scale, m, s);
+                    else online(v, valid, p.scale, m, s);
+                    const int32_t l = label - col;
+                    if (__any_sync(~0u, l >= 0 && l < 32)) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) at_label = l == i ? v[i] : at_label;
+                    }
+                } else if (WHAT == kGrad) {
+                    const int32_t valid = row < units.rows ? p.V - col : 0, l = label - col;
+                    const float gs = p.grad_scale;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = exp2_fast(fmaf(v[i], p.scale, -lse2)) * gs;
+                    if (__any_sync(~0u, l >= 0 && l < 32)) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = l == i ? v[i] - gs : v[i];
+                    }
+                    if (__any_sync(~0u, valid < 32)) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = i < valid ? v[i] : 0.0f;
+                    }
+                    T *o = (T *)p.grad + (int64_t)row * p.piece + col;
+                    uint32_t r[8];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) r[i] = pack2(v[h * 16 + 2 * i], v[h * 16 + 2 * i + 1], T());
+                        store32(o + h * 16, r);
+                    }
+                } else if (t.dw) {
+                    put_weight_grad<T>(p, row, col, v, unscale);
+                } else if (row < units.rows && col < p.Dp && (t.blocks > 0 || p.first)) {
+                    float *o = p.acc + ((int64_t)t.part * units.rows + row) * p.Dp + col;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        if (!p.first) {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const float4 y = reinterpret_cast<const float4 *>(o + h * 8)[i];
+                                v[h * 8 + i * 4] += y.x; v[h * 8 + i * 4 + 1] += y.y; v[h * 8 + i * 4 + 2] += y.z; v[h * 8 + i * 4 + 3] += y.w;
+                            }
+                        }
+                        uint32_t r[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[h * 8 + i]);
+                        store32(o + h * 8, r);
+                    }
+                }
+            }
+            if (WHAT == kLoss && row < units.rows) {
+                p.part[(int64_t)row * p.part_pitch + (c0 >> 7)] = make_float2(m, s);
+                if (label >= c0 && label < c0 + 128) p.hit[row] = at_label * (p.scale * 0.6931471805599453f);
+            }
+            if (t.blocks > 0) {
+                tc_before_sync();
+                __syncwarp();
+                if (lane == 0) bar_arrive_in_cluster(in_cta(smem_u32(&taken[buf]), 0));
+                buf ^= 1;
+                buf_phase ^= buf == 0;
+            }
         }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int d = 8; d; d >>= 1) {
-            const float om = __shfl_xor_sync(~0u, m[i], d), os = __shfl_xor_sync(~0u, s[i], d), n = fmaxf(m[i], om);
-            s[i] = (m[i] == -INFINITY ? s[i] : s[i] * __expf(m[i] - n)) + (om == -INFINITY ? os : os * __expf(om - n));
-            m[i] = n;
-        }
-        if (tx == 0 && i0 + ty * 4 + i < L) part[(i0 + ty * 4 + i) * tiles_v + t] = make_float2(m[i], s[i]);
-    }
+    __syncwarp();
+    tc_before_sync();
+    __syncthreads();
+    if (*gave_up) __nanosleep(1000000);       // copies that are still on their way land before the shared memory goes
+    cluster_sync();
+    tc_after_sync();
+    if (warp == 2) tmem_free(tmem, 512);
 }
 
-template <class T>
-__global__ void __launch_bounds__(256) grad_kernel(const Head *head, const T *h, int64_t hs, const T *w, int64_t ws, const int32_t *label, const float *lse,
-                                                   const float *dloss, int64_t v0, int64_t nv, int64_t D, float scale, T *g, int64_t gs)
+// ---- launches ----------------------------------------------------------------------------------------------------------------
+
+// Pairs of CTAs that the device holds at once; 0 on an error.  Also allows the kernels their shared memory.
+template <class T> int32_t pairs_on_device()
 {
-    DCT_SHARED;
-    const int64_t L = head->rows, i0 = (int64_t)blockIdx.y * kS, j0 = (int64_t)blockIdx.x * kS;
-    if (i0 >= L) return;
-    tile_product(c, h, hs, 1, i0, L, w, ws, 1, j0, nv, D, sa, sb);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = i0 + ty * 4 + i, v = j0 + tx * 4 + j;
-            float x = 0.0f;
-            if (r < L && v < nv) x = (__expf(c[i][j] * scale - lse[r]) - (label[r] == v0 + v ? 1.0f : 0.0f)) * (dloss[r] * head->grad_scale);
-            g[r * gs + v] = from_f<T>(x);
-        }
+    static int32_t cached[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    const int32_t have = __atomic_load_n(&cached[dev], __ATOMIC_ACQUIRE);
+    if (have) return have;
+    for (auto f : {vocab_product<T, kLoss>, vocab_product<T, kGrad>, vocab_product<T, kBack>})
+        if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) != cudaSuccess) return 0;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3((unsigned)sm_count() & ~1u);
+    c.blockDim = dim3(kTcThreads);
+    c.dynamicSmemBytes = kTcSmem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    c.attrs = at;
+    c.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, vocab_product<T, kLoss>, &c) != cudaSuccess || n <= 0) return 0;
+    __atomic_store_n(&cached[dev], n, __ATOMIC_RELEASE);
+    return n;
 }
 
-template <class T, class O>
-__global__ void __launch_bounds__(256) weight_grad_kernel(const Head *head, const T *g, int64_t gs, const T *h, int64_t hs, int64_t nv, int64_t D, O *dw,
-                                                          int64_t dws, bool accumulate)
+template <class T> constexpr bool is_bf16() { return __is_same(T, __nv_bfloat16); }
+
+// g carries 2^14 in fp16, so that probabilities down to 2^-28 stay normal numbers; bf16 has fp32's range
+template <class T> constexpr float grad_scale() { return is_bf16<T>() ? 1.0f : 16384.0f; }
+
+template <class T, int WHAT>
+int launch_units(int64_t most_units, int32_t pairs, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &a_dw, const CUtensorMap &b_dw, const Product &p,
+                 cudaStream_t st)
 {
-    DCT_SHARED;
-    const int64_t L = head->rows, i0 = (int64_t)blockIdx.y * kS, j0 = (int64_t)blockIdx.x * kS;
-    tile_product(c, g, 1, gs, i0, nv, h, 1, hs, j0, D, L, sa, sb);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t v = i0 + ty * 4 + i, d = j0 + tx * 4 + j;
-            if (v >= nv || d >= D) continue;
-            O *o = dw + v * dws + d;
-            *o = from_f<O>((accumulate ? to_f(*o) : 0.0f) + c[i][j] * head->grad_unscale);
-        }
-}
-
-template <class T>
-__global__ void __launch_bounds__(256) hidden_grad_kernel(const Head *head, const T *g, int64_t gs, const T *w, int64_t ws, int64_t nv, int64_t D, float *acc,
-                                                          int64_t as, bool first)
-{
-    DCT_SHARED;
-    const int64_t L = head->rows, i0 = (int64_t)blockIdx.y * kS, j0 = (int64_t)blockIdx.x * kS;
-    if (i0 >= L) return;
-    tile_product(c, g, gs, 1, i0, L, w, 1, ws, j0, D, nv, sa, sb);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = i0 + ty * 4 + i, d = j0 + tx * 4 + j;
-            if (r >= L || d >= D) continue;
-            float *o = acc + r * as + d;
-            *o = (first ? 0.0f : *o) + c[i][j];
-        }
-}
-#undef DCT_SHARED
-
-// ---- launches -------------------------------------------------------------------------------------------------------------
-
-inline dim3 tiles(int64_t x, int64_t y, int s) { return dim3((unsigned)ceil_div(x, s), (unsigned)ceil_div(y, kS)); }
-
-template <class T>
-int loss_product(const Head *head, const void *rows, int64_t rs, const void *w, int64_t ws, const int32_t *label, int64_t N, int64_t V, int64_t D, float scale,
-                 float2 *part, float *hit, int32_t tiles_v, cudaStream_t st)
-{
-    loss_kernel<T><<<tiles(V, N, kTileN), 256, 0, st>>>(head, (const T *)rows, rs, (const T *)w, ws, label, V, D, scale, part, hit, tiles_v);
-    return launched();
-}
-
-template <class T>
-int grad_product(const Head *head, const void *rows, int64_t rs, const void *w, int64_t ws, const int32_t *label, const float *lse, const float *dloss, int64_t N,
-                 int64_t v0, int64_t nv, int64_t D, float scale, void *g, int64_t gs, cudaStream_t st)
-{
-    grad_kernel<T><<<tiles(nv, N, kS), 256, 0, st>>>(head, (const T *)rows, rs, (const T *)w, ws, label, lse, dloss, v0, nv, D, scale, (T *)g, gs);
-    return launched();
-}
-
-template <class T>
-int back_products(const Head *head, const void *g, int64_t gs, const void *rows, int64_t rs, const void *w, int64_t ws, int64_t N, int64_t nv, int64_t D,
-                  void *dw, int64_t dws, bool dw_f32, bool accumulate, float *acc, int64_t as, int32_t, int32_t, bool first, cudaStream_t st)
-{
-    if (dw && dw_f32) weight_grad_kernel<T, float><<<tiles(D, nv, kS), 256, 0, st>>>(head, (const T *)g, gs, (const T *)rows, rs, nv, D, (float *)dw, dws, accumulate);
-    if (dw && !dw_f32) weight_grad_kernel<T, T><<<tiles(D, nv, kS), 256, 0, st>>>(head, (const T *)g, gs, (const T *)rows, rs, nv, D, (T *)dw, dws, accumulate);
-    if (acc) hidden_grad_kernel<T><<<tiles(D, N, kS), 256, 0, st>>>(head, (const T *)g, gs, (const T *)w, ws, nv, D, acc, as, first);
+    const int64_t n = most_units < pairs ? most_units : pairs;
+    vocab_product<T, WHAT><<<(unsigned)(2 * (n > 0 ? n : 1)), kTcThreads, kTcSmem, st>>>(a, b, a_dw, b_dw, p);
     return launched();
 }
 

@@ -3,8 +3,9 @@
 //
 // With h the labelled rows and W the weight, the logits l = c h W^T of a tile live in registers only:
 //   forward   per (row, tile of the vocabulary) the maximum and the sum of exp(l - maximum) leave the kernel; lse joins them
-//   backward  per piece of the vocabulary l is formed again, g = (exp(l - lse) - [label]) dloss c is kept in 16 bits,
-//             then dW = g^T h and dh += g W
+//   backward  per piece of the vocabulary l is formed again and g = exp(l - lse) - [label] is kept in 16 bits; then, with
+//             f = dloss c of each row,  dW = g^T (f h)  and  dh = f (g W)
+// The factors f stay out of g: next to the label g is near -1, where 16 bits are finest, and f meets dh in fp32.
 // Rows without a label are taken out first (vocab_gather), so the products run over labelled rows alone and whatever the
 // others hold never meets a product.
 #include "train_common.cuh"
@@ -12,7 +13,7 @@
 
 namespace dct {
 
-constexpr int kGatherRows = 32;
+constexpr int kGatherBlocks = 256;
 
 // ---- taking out the labelled rows ------------------------------------------------------------------------------------------
 
@@ -21,92 +22,102 @@ struct Gather {
     const int64_t *targets; int64_t ignore;
     const float *lse, *dloss;              // backward only
     int64_t N, V; int32_t D, Dp;
+    int32_t per_block;                     // rows of a block, a multiple of 32
     float logit_scale;
-    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_dloss;
-    void *rows;                            // [Lp][Dp]
+    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_factor;
+    void *rows, *scaled;                   // [Lp][Dp]: h, and for dW h times its row's factor over the largest one
     float *loss_out, *lse_out;             // forward only: rows without a label are written here
-    int32_t scale_grad;                    // whether g needs a power of two (fp16)
+    int32_t vocab_blocks, pairs; int64_t acc_rows;
 };
 
+// Every block counts the labelled rows before its own, and in the backward pass finds the largest factor |dloss c|, by itself:
+// a few bytes per row from L2, and no block waits for another.  Dividing the factors by the largest one keeps h' at the size of
+// h, and equal to it where all rows weigh the same (a mean over tokens): then h' is not rounded again.
 template <class T, int V>
 __global__ void __launch_bounds__(256) vocab_gather(Gather a)
 {
     __shared__ int32_t count[8];
     __shared__ float top[8];
-    __shared__ int32_t where[kGatherRows];
+    __shared__ int32_t where[32];
+    __shared__ float ratio[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t first = (int64_t)blockIdx.x * kGatherRows;
+    const int64_t first = (int64_t)blockIdx.x * a.per_block, end = min(a.N, first + a.per_block);
     const bool last_block = blockIdx.x == gridDim.x - 1;
-    // labelled rows before this block's, and for the last block the largest |dloss|: every block reads what it needs itself
     int32_t c = 0;
     float m = 0.0f;
-    for (int64_t i = tid; i < first; i += 256) {
+    const int64_t look = a.dloss ? a.N : first;
+#pragma unroll 4
+    for (int64_t i = tid; i < look; i += 256) {
         const int64_t t = a.targets[i];
         const bool ok = t != a.ignore && t >= 0 && t < a.V;
-        c += ok;
-        if (last_block && a.dloss && ok) m = fmaxf(m, fabsf(a.dloss[i]));
+        const float d = a.dloss ? a.dloss[i] : 0.0f;
+        c += ok && i < first;
+        m = ok ? fmaxf(m, fabsf(d * a.logit_scale)) : m;
     }
     c = __reduce_add_sync(~0u, c);
-    if (lane == 0) count[warp] = c;
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    if (lane == 0) { count[warp] = c; top[warp] = m; }
     __syncthreads();
     int32_t base = 0;
-    for (int w = 0; w < 8; ++w) base += count[w];
-    int32_t labelled = 0;
-    if (warp == 0) {
-        const int64_t i = first + lane;
-        const int64_t t = i < a.N ? a.targets[i] : a.ignore;
-        const bool ok = i < a.N && t != a.ignore && t >= 0 && t < a.V;
+    m = 0.0f;
+    for (int w = 0; w < 8; ++w) { base += count[w]; m = fmaxf(m, top[w]); }
+    if (!(m > 0.0f && m < INFINITY)) m = 1.0f;
+    const T *hidden = (const T *)a.hidden;
+    T *rows = (T *)a.rows, *scaled = (T *)a.scaled;
+    for (int64_t i0 = first; i0 < end; i0 += 32) {
+        // each warp finds the places of all 32 rows, one of them writes what belongs to a row
+        const int64_t i = i0 + lane;
+        const int64_t t = i < end ? a.targets[i] : a.ignore;
+        const bool ok = t != a.ignore && t >= 0 && t < a.V;
         const uint32_t all = __ballot_sync(~0u, ok);
         const int32_t p = base + __popc(all & ((1u << lane) - 1));
-        where[lane] = ok ? p : -1;
-        if (i < a.N) {
-            a.pos_of[i] = ok ? p : -1;
-            if (!ok && a.loss_out) a.loss_out[i] = a.lse_out[i] = t == a.ignore ? 0.0f : __uint_as_float(0x7fffffffu);
-        }
-        if (ok) {
-            a.row_of[p] = (int32_t)i;
-            a.label[p] = (int32_t)t;
-            if (a.dloss) {
-                a.row_lse[p] = a.lse[i];
-                a.row_dloss[p] = a.dloss[i] * a.logit_scale;
-                m = fmaxf(m, fabsf(a.dloss[i]));
+        if (warp == 0) {
+            where[lane] = ok ? p : -1;
+            if (i < end) {
+                a.pos_of[i] = ok ? p : -1;
+                if (!ok && a.loss_out) a.loss_out[i] = a.lse_out[i] = t == a.ignore ? 0.0f : __uint_as_float(0x7fffffffu);
+            }
+            if (ok) {
+                a.row_of[p] = (int32_t)i;
+                a.label[p] = (int32_t)t;
+                if (a.dloss) {
+                    const float f = a.dloss[i] * a.logit_scale;
+                    a.row_lse[p] = a.lse[i];
+                    a.row_factor[p] = f;
+                    ratio[lane] = f / m;
+                }
             }
         }
-        labelled = __popc(all);
-    }
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-    if (lane == 0) top[warp] = m;
-    __syncthreads();
-    if (last_block && tid == 0) {
-        for (int w = 0; w < 8; ++w) m = fmaxf(m, top[w]);
-        m *= fabsf(a.logit_scale);
-        // |g| <= 2^14 in fp16, whatever dloss is: probabilities down to 2^-28 of it stay normal numbers
-        int e = 0;
-        if (a.scale_grad && m > 0.0f && m < INFINITY) e = min(max(13 - ilogbf(m), -100), 100);
-        a.head->rows = base + labelled;
-        a.head->grad_scale = ldexpf(1.0f, e);
-        a.head->grad_unscale = ldexpf(1.0f, -e);
-    }
-    const T *hidden = (const T *)a.hidden;
-    T *rows = (T *)a.rows;
-    for (int j = warp; j < kGatherRows; j += 8) {
-        const int32_t p = where[j];
-        if (p < 0) continue;
-        const T *from = hidden + (first + j) * a.hs;
-        T *to = rows + (int64_t)p * a.Dp;
-        for (int32_t d = lane * V; d < a.Dp; d += 32 * V) {
-            Pack<T, V> x = {};
-            if (d < a.D) x = *reinterpret_cast<const Pack<T, V> *>(from + d);
-            *reinterpret_cast<Pack<T, V> *>(to + d) = x;
-        }
-    }
-    if (last_block) {
-        // the product over rows takes whole blocks of kRowBlock: what follows the last row there is zero
-        __shared__ int32_t total;
-        if (tid == 0) total = base + labelled;
+        base += __popc(all);
         __syncthreads();
-        const int64_t from = (int64_t)total * a.Dp, to = ceil_div(total, kRowBlock) * kRowBlock * (int64_t)a.Dp;
-        for (int64_t d = from + tid * 8; d < to; d += 256 * 8) *reinterpret_cast<uint4 *>(rows + d) = make_uint4(0, 0, 0, 0);
+        for (int j = warp; j < 32; j += 8) {
+            const int32_t to = where[j];
+            if (to < 0) continue;
+            const T *from = hidden + (i0 + j) * a.hs;
+            const float f = scaled ? ratio[j] : 0.0f;
+            for (int32_t d = lane * V; d < a.Dp; d += 32 * V) {
+                Pack<T, V> x = {};
+                if (d < a.D) x = *reinterpret_cast<const Pack<T, V> *>(from + d);
+                *reinterpret_cast<Pack<T, V> *>(rows + (int64_t)to * a.Dp + d) = x;
+                if (scaled) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) x.v[k] = from_f<T>(to_f(x.v[k]) * f);
+                    *reinterpret_cast<Pack<T, V> *>(scaled + (int64_t)to * a.Dp + d) = x;
+                }
+            }
+        }
+        __syncthreads();
+    }
+    if (!last_block) return;
+    if (tid == 0) {
+        a.head->rows = base;
+        a.head->top = m;
+        a.head->parts = a.dloss ? parts_of((uint32_t)base, (uint32_t)a.D, (uint32_t)a.vocab_blocks, (uint32_t)a.pairs, a.acc_rows) : 1;
+    }
+    // dW is summed over whole blocks of kRowBlock rows: what follows the last row there is zero
+    if (scaled) {
+        const int64_t from = (int64_t)base * a.Dp, to = ceil_div(base, kRowBlock) * kRowBlock * (int64_t)a.Dp;
+        for (int64_t d = from + tid * 8; d < to; d += 256 * 8) *reinterpret_cast<uint4 *>(scaled + d) = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -127,21 +138,20 @@ __global__ void __launch_bounds__(256) vocab_join(const Head *__restrict__ head,
     const int64_t j = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (j >= head->rows) return;
     const float2 *p = part + j * tiles;
-    float m = -INFINITY, s = 0.0f;
-    for (int32_t t = lane; t < tiles; t += 32) {
-        const float2 x = p[t];
-        const float n = fmaxf(m, x.x);
+    float m = -INFINITY, s = 0.0f;                          // in powers of two, as the tiles are
+    auto add = [&](float om, float os) {
+        const float n = fmaxf(m, om);
         // a maximum of -inf stands for a part without a finite logit; its sum is 0, or NaN if it holds one
-        s = (m == -INFINITY ? s : s * __expf(m - n)) + (x.x == -INFINITY ? x.y : x.y * __expf(x.x - n));
+        s = (m == -INFINITY ? s : s * exp2_fast(m - n)) + (om == -INFINITY ? os : os * exp2_fast(om - n));
         m = n;
-    }
+    };
+    for (int32_t t = lane; t < tiles; t += 32) add(p[t].x, p[t].y);
     for (int d = 16; d; d >>= 1) {
-        const float om = __shfl_xor_sync(~0u, m, d), os = __shfl_xor_sync(~0u, s, d), n = fmaxf(m, om);
-        s = (m == -INFINITY ? s : s * __expf(m - n)) + (om == -INFINITY ? os : os * __expf(om - n));
-        m = n;
+        const float om = __shfl_xor_sync(~0u, m, d), os = __shfl_xor_sync(~0u, s, d);
+        add(om, os);
     }
     if (lane == 0) {
-        const float z = m + logf(s);
+        const float z = (m + log2f(s)) * 0.6931471805599453f;
         lse[row_of[j]] = z;
         loss[row_of[j]] = z - hit[j];
     }
@@ -149,30 +159,36 @@ __global__ void __launch_bounds__(256) vocab_join(const Head *__restrict__ head,
 
 // ---- the gradient of the hidden states: partial products joined in order and put back to their rows ------------------------
 
-template <class T>
-__global__ void __launch_bounds__(256) vocab_put_back(const Head *__restrict__ head, const int32_t *__restrict__ pos_of, const float *__restrict__ acc,
-                                                      int64_t N, int32_t D, int32_t Dp, int32_t tiles_d, int32_t vocab_blocks, T *__restrict__ out, int64_t os)
+template <class T, int V>
+__global__ void __launch_bounds__(256) vocab_put_back(const Head *__restrict__ head, const int32_t *__restrict__ pos_of, const float *__restrict__ factor,
+                                                      const float *__restrict__ acc, int64_t N, int32_t D, int32_t Dp, float unscale, T *__restrict__ out, int64_t os)
 {
     const int64_t n = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (n >= N) return;
-    const int32_t p = pos_of[n], rows = head->rows, parts = split_of(rows, tiles_d, vocab_blocks);
-    const float unscale = head->grad_unscale;
-    for (int32_t d = threadIdx.x & 31; d < D; d += 32) {
-        float s = 0.0f;
-        if (p >= 0) {
-            for (int32_t k = 0; k < parts; ++k) s += acc[((int64_t)k * rows + p) * Dp + d];
-            s *= unscale;
-        }
-        out[n * os + d] = from_f<T>(s);
+    const int32_t p = pos_of[n], rows = head->rows, parts = head->parts;
+    const float f = p >= 0 ? factor[p] * unscale : 0.0f;
+    for (int32_t d = (threadIdx.x & 31) * V; d < D; d += 32 * V) {
+        Pack<T, V> o;
+        float s[V] = {};
+        if (p >= 0)
+            for (int32_t k = 0; k < parts; ++k) {
+                const Pack<float, V> x = *reinterpret_cast<const Pack<float, V> *>(acc + ((int64_t)k * rows + p) * Dp + d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[i] += x.v[i];
+            }
+#pragma unroll
+        for (int i = 0; i < V; ++i) o.v[i] = from_f<T>(p >= 0 ? s[i] * f : 0.0f);
+        *reinterpret_cast<Pack<T, V> *>(out + n * os + d) = o;
     }
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------------
 
 struct Plan {
-    int32_t Dp, tiles_v, tiles_d, piece, pieces;   // piece: columns of the vocabulary that g holds at a time
+    int32_t Dp, tiles_v, piece, pieces, vocab_blocks;   // piece: columns of the vocabulary that g holds at a time
+    int64_t Lp, acc_rows;
     bool copy_weight;
-    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_dloss, *hit; float2 *part; char *rows, *weight, *grad; float *acc;
+    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_factor, *hit; float2 *part; char *rows, *scaled, *weight, *grad; float *acc;
     size_t bytes;
 };
 
@@ -181,29 +197,31 @@ inline Plan make_plan(void *base, int64_t N, int64_t V, int64_t D, const void *w
     Plan p{};
     char *b = (char *)base;
     size_t at = 0;
-    auto take = [&](size_t bytes) { char *r = b + at; at += align_up(bytes, 1024); return r; };
-    const int64_t Lp = ceil_div(N > 0 ? N : 1, kTileM) * kTileM;
-    p.Dp = (int32_t)(ceil_div(D, 64) * 64);
+    auto take = [&](size_t bytes) { char *r = b + at; at += align_up(bytes, 256); return r; };
+    p.Lp = ceil_div(N > 0 ? N : 1, kTileM) * kTileM;
+    p.Dp = (int32_t)(ceil_div(D, kRowBlock) * kRowBlock);
     p.tiles_v = (int32_t)ceil_div(V, kTileN);
-    p.tiles_d = (int32_t)ceil_div(D, kTileN);
     p.copy_weight = !rows_on(weight, ws, 2, 16);
     p.head = (Head *)take(sizeof(Head));
-    p.row_of = (int32_t *)take(Lp * 4);
-    p.pos_of = (int32_t *)take(Lp * 4);
-    p.label = (int32_t *)take(Lp * 4);
-    p.rows = take((size_t)Lp * p.Dp * 2);
+    p.row_of = (int32_t *)take(p.Lp * 4);
+    p.pos_of = (int32_t *)take(p.Lp * 4);
+    p.label = (int32_t *)take(p.Lp * 4);
+    p.rows = take((size_t)p.Lp * p.Dp * 2);
     if (p.copy_weight) p.weight = take((size_t)V * p.Dp * 2);
     if (!backward) {
-        p.hit = (float *)take(Lp * 4);
-        p.part = (float2 *)take((size_t)Lp * p.tiles_v * 8);
+        p.hit = (float *)take(p.Lp * 4);
+        p.part = (float2 *)take((size_t)p.Lp * p.tiles_v * 16);
     } else {
-        p.row_lse = (float *)take(Lp * 4);
-        p.row_dloss = (float *)take(Lp * 4);
-        const int64_t most = kPieceBytes / (2 * Lp) / kTileM * kTileM, whole = ceil_div(V, kTileM) * kTileM;
+        p.row_lse = (float *)take(p.Lp * 4);
+        p.row_factor = (float *)take(p.Lp * 4);
+        p.scaled = take((size_t)p.Lp * p.Dp * 2);
+        const int64_t most = kPieceBytes / (2 * p.Lp) / kTileM * kTileM, whole = ceil_div(V, kTileM) * kTileM;
         p.piece = (int32_t)(most < kTileM ? kTileM : most < whole ? most : whole);
         p.pieces = (int32_t)ceil_div(V, p.piece);
-        p.grad = take((size_t)Lp * p.piece * 2);
-        p.acc = (float *)take((size_t)acc_rows(N, p.tiles_d) * p.Dp * 4);
+        p.vocab_blocks = (int32_t)ceil_div(V < p.piece ? V : p.piece, kRowBlock);
+        p.grad = take((size_t)p.Lp * p.piece * 2);
+        p.acc_rows = acc_rows_for(N, D);
+        p.acc = (float *)take((size_t)p.acc_rows * p.Dp * 4);
     }
     p.bytes = at;
     return p;
@@ -213,6 +231,8 @@ inline int check(const void *hidden, int64_t hs, const void *weight, int64_t ws,
 {
     if (N < 0 || V <= 0 || D <= 0) return DC_ERR_SHAPE;
     if (N > kMaxDim || V > kMaxDim || D > kMaxDim) return DC_ERR_RANGE;
+    const int64_t tm = ceil_div(N, kTileM), tv = ceil_div(V, kTileM), td = ceil_div(D, kTileM), most = INT32_MAX / 2;   // tiles are counted in 32 bits
+    if (tm * tv > most || tv * td > most || tm * td > most / kMaxParts) return DC_ERR_RANGE;
     if (dtype != DC_BF16 && dtype != DC_F16) return DC_ERR_UNSUPPORTED;
     if (N == 0) return DC_OK;
     if (!hidden || !weight || !targets) return DC_ERR_NULL;
@@ -222,46 +242,83 @@ inline int check(const void *hidden, int64_t hs, const void *weight, int64_t ws,
 }
 
 template <class T>
-int gather(const Gather &g, cudaStream_t st)
+int gather(Gather &g, cudaStream_t st)
 {
-    const unsigned blocks = (unsigned)ceil_div(g.N, kGatherRows);
+    g.per_block = (int32_t)(ceil_div(ceil_div(g.N, kGatherBlocks), 32) * 32);
+    const unsigned blocks = (unsigned)ceil_div(g.N, g.per_block);
     if (g.D % 8 == 0 && rows_on(g.hidden, g.hs, 2, 16)) vocab_gather<T, 8><<<blocks, 256, 0, st>>>(g);
     else vocab_gather<T, 1><<<blocks, 256, 0, st>>>(g);
     return launched();
 }
 
+// The weight as bulk tensor copies can read it.
+template <class T>
+void readable(const Plan &p, const Gather &g, const void **weight, int64_t *ws, cudaStream_t st)
+{
+    if (!p.copy_weight) return;
+    vocab_copy_weight<T><<<(unsigned)(sm_count() * 8), 256, 0, st>>>((const T *)*weight, *ws, g.V, g.D, p.Dp, (T *)p.weight);
+    *weight = p.weight;
+    *ws = p.Dp;
+}
+
 template <class T>
 int forward(Gather g, const Plan &p, const void *weight, int64_t ws, float *loss, float *lse, cudaStream_t st)
 {
+    constexpr bool bf = is_bf16<T>();
+    const int32_t pairs = pairs_on_device<T>();
+    if (pairs == 0) return DC_ERR_CUDA;
+    CUtensorMap a, b;
+    Product q{};
+    if (!tensor_map(&a, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&b, p.copy_weight ? p.weight : weight, bf, g.D, g.V, p.copy_weight ? p.Dp : ws, 128))
+        return DC_ERR_CUDA;
     if (int e = gather<T>(g, st)) return e;
-    if (p.copy_weight) {
-        vocab_copy_weight<T><<<(unsigned)(sm_count() * 8), 256, 0, st>>>((const T *)weight, ws, g.V, g.D, p.Dp, (T *)p.weight);
-        weight = p.weight;
-        ws = p.Dp;
-    }
-    if (int e = loss_product<T>(p.head, p.rows, p.Dp, weight, ws, p.label, g.N, g.V, g.D, g.logit_scale, p.part, p.hit, p.tiles_v, st)) return e;
-    vocab_join<<<(unsigned)ceil_div(g.N, 8), 256, 0, st>>>(p.head, p.row_of, p.part, p.hit, p.tiles_v, loss, lse);
+    readable<T>(p, g, &weight, &ws, st);
+    q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.part = p.part; q.hit = p.hit; q.part_pitch = 2 * p.tiles_v;
+    q.V = (int32_t)g.V; q.D = g.D; q.Dp = p.Dp;
+    if (int e = launch_units<T, kLoss>(p.Lp / kTileM * p.tiles_v, pairs, a, b, a, b, q, st)) return e;
+    vocab_join<<<(unsigned)ceil_div(g.N, 8), 256, 0, st>>>(p.head, p.row_of, p.part, p.hit, 2 * p.tiles_v, loss, lse);
     return launched();
 }
 
 template <class T>
 int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, int64_t dhs, void *dw, int64_t dws, bool dw_f32, bool accumulate, cudaStream_t st)
 {
+    constexpr bool bf = is_bf16<T>();
+    const int32_t pairs = pairs_on_device<T>();
+    if (pairs == 0) return DC_ERR_CUDA;
+    g.vocab_blocks = p.vocab_blocks; g.pairs = pairs; g.acc_rows = p.acc_rows;
+    if (!dw) g.scaled = nullptr;
     if (int e = gather<T>(g, st)) return e;
-    if (p.copy_weight) {
-        vocab_copy_weight<T><<<(unsigned)(sm_count() * 8), 256, 0, st>>>((const T *)weight, ws, g.V, g.D, p.Dp, (T *)p.weight);
-        weight = p.weight;
-        ws = p.Dp;
-    }
+    readable<T>(p, g, &weight, &ws, st);
+    const int ob = dw_f32 ? 4 : 2;
+    CUtensorMap rows, grad_k, grad_mn, scaled_mn;
+    if (!tensor_map(&rows, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&grad_k, p.grad, bf, p.piece, p.Lp, p.piece, 128) ||
+        !tensor_map(&grad_mn, p.grad, bf, p.piece, p.Lp, p.piece, 64) || !tensor_map(&scaled_mn, p.scaled, bf, p.Dp, p.Lp, p.Dp, 64))
+        return DC_ERR_CUDA;
+    const int64_t tm = p.Lp / kTileM, td = ceil_div(g.D, kTileN);
     for (int32_t k = 0; k < p.pieces; ++k) {
         const int64_t v0 = (int64_t)k * p.piece, nv = g.V - v0 < p.piece ? g.V - v0 : p.piece;
         const T *w = (const T *)weight + v0 * ws;
-        if (int e = grad_product<T>(p.head, p.rows, p.Dp, w, ws, p.label, p.row_lse, p.row_dloss, g.N, v0, nv, g.D, g.logit_scale, p.grad, p.piece, st)) return e;
-        char *dwk = dw ? (char *)dw + v0 * dws * (dw_f32 ? 4 : 2) : nullptr;
-        if (int e = back_products<T>(p.head, p.grad, p.piece, p.rows, p.Dp, w, ws, g.N, nv, g.D, dwk, dws, dw_f32, accumulate, dh ? p.acc : nullptr,
-                                     p.Dp, p.tiles_d, p.piece / kRowBlock, k == 0, st)) return e;
+        CUtensorMap w_k, w_mn;
+        if (!tensor_map(&w_k, w, bf, g.D, nv, ws, 128) || !tensor_map(&w_mn, w, bf, g.D, nv, ws, 64)) return DC_ERR_CUDA;
+        Product q{};
+        q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.lse = p.row_lse; q.grad = p.grad; q.piece = p.piece;
+        q.v0 = (int32_t)v0; q.V = (int32_t)nv; q.D = g.D; q.Dp = p.Dp; q.grad_scale = grad_scale<T>();
+        if (int e = launch_units<T, kGrad>(tm * ceil_div(nv, kTileN), pairs, rows, w_k, rows, w_k, q, st)) return e;
+        if (dw) {
+            q.dw = (char *)dw + v0 * dws * ob;
+            q.dw_stride = dws; q.dw_f32 = dw_f32; q.dw_add = accumulate; q.dw_wide = rows_on(dw, dws, ob, 16);
+        }
+        q.acc = dh ? p.acc : nullptr;
+        q.first = k == 0; q.vocab_blocks = p.vocab_blocks; q.grad_scale = 1.0f / grad_scale<T>();
+        const int64_t units = (dw ? ceil_div(nv, kTileM) * td : 0) + (dh ? tm * td * kMaxParts : 0);
+        if (int e = launch_units<T, kBack>(units, pairs, grad_k, w_mn, grad_mn, scaled_mn, q, st)) return e;
     }
-    if (dh) vocab_put_back<T><<<(unsigned)ceil_div(g.N, 8), 256, 0, st>>>(p.head, p.pos_of, p.acc, g.N, g.D, p.Dp, p.tiles_d, p.piece / kRowBlock, (T *)dh, dhs);
+    if (!dh) return DC_OK;
+    const unsigned blocks = (unsigned)ceil_div(g.N, 8);
+    const float unscale = 1.0f / grad_scale<T>();
+    if (g.D % 4 == 0 && rows_on(dh, dhs, 2, 8)) vocab_put_back<T, 4><<<blocks, 256, 0, st>>>(p.head, p.pos_of, p.row_factor, p.acc, g.N, g.D, p.Dp, unscale, (T *)dh, dhs);
+    else vocab_put_back<T, 1><<<blocks, 256, 0, st>>>(p.head, p.pos_of, p.row_factor, p.acc, g.N, g.D, p.Dp, unscale, (T *)dh, dhs);
     return launched();
 }
 
@@ -318,7 +375,7 @@ extern "C" int dc_vocab_loss_backward(const void *hidden, int64_t hidden_stride,
     Gather g{};
     g.hidden = hidden; g.hs = hidden_stride; g.targets = targets; g.ignore = ignore_index; g.lse = lse; g.dloss = dloss; g.N = N; g.V = V;
     g.D = (int32_t)D; g.Dp = p.Dp; g.logit_scale = logit_scale; g.head = p.head; g.row_of = p.row_of; g.pos_of = p.pos_of; g.label = p.label;
-    g.row_lse = p.row_lse; g.row_dloss = p.row_dloss; g.rows = p.rows; g.scale_grad = dtype == DC_F16;
+    g.row_lse = p.row_lse; g.row_factor = p.row_factor; g.rows = p.rows; g.scaled = p.scaled;
     return dtype == DC_BF16
                ? backward<__nv_bfloat16>(g, p, weight, weight_stride, dhidden, dhidden_stride, dweight, dweight_stride, dweight_dtype == DC_F32, accumulate != 0, st)
                : backward<__half>(g, p, weight, weight_stride, dhidden, dhidden_stride, dweight, dweight_stride, dweight_dtype == DC_F32, accumulate != 0, st);

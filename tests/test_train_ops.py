@@ -286,7 +286,9 @@ def check_backward(api, h, w, t, dloss, lse, e, span, ignore=-100, c=1.0, dw_dty
     bh[rows] = eg @ wd.abs() + (V + 64) * 2.0 ** -22 * (g.abs() @ wd.abs())
     close(dh, wdh, bh + plain.ROUND[dt] * 1.01 * wdh.abs() + plain.TINY[dt], "dhidden")
     out = dw.dtype
-    bw = eg.t() @ hd.abs() + (len(rows) + 64) * 2.0 ** -22 * (g.abs().t() @ hd.abs())
+    # the rows' weights are brought into h before the product, which rounds it to 16 bits once more
+    bw = eg.t() @ hd.abs() + ((len(rows) + 64) * 2.0 ** -22 + plain.ROUND[dt] * 1.01) * (g.abs().t() @ hd.abs())
+    bw = bw + (amax * 2.0 ** -25 * (g / d).abs().sum(0)[:, None] if dt == F16 else 0.0)
     close(dw, wdw, bw + plain.ROUND[out] * 1.01 * wdw.abs() + plain.TINY[out], "dweight")
     return dh, dw, wdw, bw
 
