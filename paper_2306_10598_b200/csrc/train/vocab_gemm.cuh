@@ -9,7 +9,7 @@
 //   what    tile of                       rows x columns      summed over        leaves as
 //   kLoss   c h W^T                       tokens x vocab      hidden             (max, sum of exp) of each row and half tile
 //   kGrad   c h W^T of a piece            tokens x vocab      hidden             g in 16 bits
-//   kBack   dW = g^T h'  of the piece     vocab x hidden      tokens             dW, added to or not
+//   kBack   dW = g^T h   of the piece     vocab x hidden      tokens             dW, added to or not
 //           dh = g W     of the piece     tokens x hidden     a part of vocab    partial products in fp32
 #pragma once
 
@@ -66,7 +66,8 @@ struct Product {
     const int32_t *label;
     float scale;                    // logit_scale * log2(e): logits in powers of two
     float2 *part; float *hit; int32_t part_pitch;
-    const float *lse;
+    const float *lse, *factor;      // of each row
+    float *rest;                    // what the label's g loses by rounding
     void *grad; int32_t piece;
     int32_t v0;                     // first of the piece
     float grad_scale;               // power of two that g carries
@@ -311,10 +312,10 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
             const int32_t c0 = t.n + half * 128;
             // what the row needs, on its way while the products run
             int32_t label = -1;
-            float lse2 = 0.0f;
+            float lse2 = 0.0f, f = 0.0f;
             if (WHAT != kBack && row < units.rows) {
                 label = p.label[row];
-                if (WHAT == kGrad) { label -= p.v0; lse2 = p.lse[row] * 1.4426950408889634f; }
+                if (WHAT == kGrad) { label -= p.v0; lse2 = p.lse[row] * 1.4426950408889634f; f = p.factor[row] * p.grad_scale; }
             }
             const float unscale = WHAT == kBack && t.dw ? p.head->top * p.grad_scale : 1.0f;
             if (t.blocks > 0) {
@@ -347,12 +348,16 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
                     }
                 } else if (WHAT == kGrad) {
                     const int32_t valid = row < units.rows ? p.V - col : 0, l = label - col;
-                    const float gs = p.grad_scale;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = exp2_fast(fmaf(v[i], p.scale, -lse2)) * gs;
+                    for (int i = 0; i < 32; ++i) v[i] = exp2_fast(fmaf(v[i], p.scale, -lse2)) * f;
                     if (__any_sync(~0u, l >= 0 && l < 32)) {
+                        float g = 0.0f;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = l == i ? v[i] - gs : v[i];
+                        for (int i = 0; i < 32; ++i) {
+                            v[i] = l == i ? v[i] - f : v[i];
+                            g = l == i ? v[i] : g;
+                        }
+                        if (l >= 0 && l < 32) p.rest[row] = g - to_f(from_f<T>(g));
                     }
                     if (__any_sync(~0u, valid < 32)) {
 #pragma unroll
@@ -438,7 +443,7 @@ template <class T> int32_t pairs_on_device()
 
 template <class T> constexpr bool is_bf16() { return __is_same(T, __nv_bfloat16); }
 
-// g carries 2^14 in fp16, so that probabilities down to 2^-28 stay normal numbers; bf16 has fp32's range
+// g in [-1, 1] carries 2^14 in fp16, so that probabilities down to 2^-28 stay normal numbers; bf16 has fp32's range
 template <class T> constexpr float grad_scale() { return is_bf16<T>() ? 1.0f : 16384.0f; }
 
 template <class T, int WHAT>

@@ -3,9 +3,11 @@
 //
 // With h the labelled rows and W the weight, the logits l = c h W^T of a tile live in registers only:
 //   forward   per (row, tile of the vocabulary) the maximum and the sum of exp(l - maximum) leave the kernel; lse joins them
-//   backward  per piece of the vocabulary l is formed again and g = exp(l - lse) - [label] is kept in 16 bits; then, with
-//             f = dloss c of each row,  dW = g^T (f h)  and  dh = f (g W)
-// The factors f stay out of g: next to the label g is near -1, where 16 bits are finest, and f meets dh in fp32.
+//   backward  per piece of the vocabulary l is formed again, g = (exp(l - lse) - [label]) f / max f, f = dloss c of each row,
+//             is kept in 16 bits, and dW = max f g^T h,  dh = max f g W
+// g lies in [-1, 1] whatever dloss is.  Its largest element in a row is the label's as a rule; what rounding takes from that
+// one is kept per row in fp32 and put back into dh, which leaves dh with little more than the rounding of the result.  dW keeps
+// it: each of its terms is off by the rounding of g, as if the result were rounded a second time.
 // Rows without a label are taken out first (vocab_gather), so the products run over labelled rows alone and whatever the
 // others hold never meets a product.
 #include "train_common.cuh"
@@ -25,21 +27,19 @@ struct Gather {
     int32_t per_block;                     // rows of a block, a multiple of 32
     float logit_scale;
     Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_factor;
-    void *rows, *scaled;                   // [Lp][Dp]: h, and for dW h times its row's factor over the largest one
+    void *rows;                            // [Lp][Dp]
     float *loss_out, *lse_out;             // forward only: rows without a label are written here
     int32_t vocab_blocks, pairs; int64_t acc_rows;
 };
 
 // Every block counts the labelled rows before its own, and in the backward pass finds the largest factor |dloss c|, by itself:
-// a few bytes per row from L2, and no block waits for another.  Dividing the factors by the largest one keeps h' at the size of
-// h, and equal to it where all rows weigh the same (a mean over tokens): then h' is not rounded again.
+// a few bytes per row from L2, and no block waits for another.
 template <class T, int V>
 __global__ void __launch_bounds__(256) vocab_gather(Gather a)
 {
     __shared__ int32_t count[8];
     __shared__ float top[8];
     __shared__ int32_t where[32];
-    __shared__ float ratio[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t first = (int64_t)blockIdx.x * a.per_block, end = min(a.N, first + a.per_block);
     const bool last_block = blockIdx.x == gridDim.x - 1;
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(256) vocab_gather(Gather a)
     for (int w = 0; w < 8; ++w) { base += count[w]; m = fmaxf(m, top[w]); }
     if (!(m > 0.0f && m < INFINITY)) m = 1.0f;
     const T *hidden = (const T *)a.hidden;
-    T *rows = (T *)a.rows, *scaled = (T *)a.scaled;
+    T *rows = (T *)a.rows;
     for (int64_t i0 = first; i0 < end; i0 += 32) {
         // each warp finds the places of all 32 rows, one of them writes what belongs to a row
         const int64_t i = i0 + lane;
@@ -81,10 +81,8 @@ __global__ void __launch_bounds__(256) vocab_gather(Gather a)
                 a.row_of[p] = (int32_t)i;
                 a.label[p] = (int32_t)t;
                 if (a.dloss) {
-                    const float f = a.dloss[i] * a.logit_scale;
                     a.row_lse[p] = a.lse[i];
-                    a.row_factor[p] = f;
-                    ratio[lane] = f / m;
+                    a.row_factor[p] = a.dloss[i] * a.logit_scale / m;
                 }
             }
         }
@@ -94,16 +92,10 @@ __global__ void __launch_bounds__(256) vocab_gather(Gather a)
             const int32_t to = where[j];
             if (to < 0) continue;
             const T *from = hidden + (i0 + j) * a.hs;
-            const float f = scaled ? ratio[j] : 0.0f;
             for (int32_t d = lane * V; d < a.Dp; d += 32 * V) {
                 Pack<T, V> x = {};
                 if (d < a.D) x = *reinterpret_cast<const Pack<T, V> *>(from + d);
                 *reinterpret_cast<Pack<T, V> *>(rows + (int64_t)to * a.Dp + d) = x;
-                if (scaled) {
-#pragma unroll
-                    for (int k = 0; k < V; ++k) x.v[k] = from_f<T>(to_f(x.v[k]) * f);
-                    *reinterpret_cast<Pack<T, V> *>(scaled + (int64_t)to * a.Dp + d) = x;
-                }
             }
         }
         __syncthreads();
@@ -115,9 +107,9 @@ __global__ void __launch_bounds__(256) vocab_gather(Gather a)
         a.head->parts = a.dloss ? parts_of((uint32_t)base, (uint32_t)a.D, (uint32_t)a.vocab_blocks, (uint32_t)a.pairs, a.acc_rows) : 1;
     }
     // dW is summed over whole blocks of kRowBlock rows: what follows the last row there is zero
-    if (scaled) {
+    if (a.dloss) {
         const int64_t from = (int64_t)base * a.Dp, to = ceil_div(base, kRowBlock) * kRowBlock * (int64_t)a.Dp;
-        for (int64_t d = from + tid * 8; d < to; d += 256 * 8) *reinterpret_cast<uint4 *>(scaled + d) = make_uint4(0, 0, 0, 0);
+        for (int64_t d = from + tid * 8; d < to; d += 256 * 8) *reinterpret_cast<uint4 *>(rows + d) = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -160,24 +152,30 @@ __global__ void __launch_bounds__(256) vocab_join(const Head *__restrict__ head,
 // ---- the gradient of the hidden states: partial products joined in order and put back to their rows ------------------------
 
 template <class T, int V>
-__global__ void __launch_bounds__(256) vocab_put_back(const Head *__restrict__ head, const int32_t *__restrict__ pos_of, const float *__restrict__ factor,
-                                                      const float *__restrict__ acc, int64_t N, int32_t D, int32_t Dp, float unscale, T *__restrict__ out, int64_t os)
+__global__ void __launch_bounds__(256) vocab_put_back(const Head *__restrict__ head, const int32_t *__restrict__ pos_of, const int32_t *__restrict__ label,
+                                                      const float *__restrict__ rest, const float *__restrict__ acc, const T *__restrict__ w, int64_t ws, int64_t N,
+                                                      int32_t D, int32_t Dp, float unscale, T *__restrict__ out, int64_t os)
 {
     const int64_t n = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (n >= N) return;
     const int32_t p = pos_of[n], rows = head->rows, parts = head->parts;
-    const float f = p >= 0 ? factor[p] * unscale : 0.0f;
+    const float f = head->top * unscale, r = p >= 0 ? rest[p] : 0.0f;
+    const T *at_label = p >= 0 ? w + label[p] * ws : w;
     for (int32_t d = (threadIdx.x & 31) * V; d < D; d += 32 * V) {
-        Pack<T, V> o;
-        float s[V] = {};
-        if (p >= 0)
+        Pack<T, V> o = {};
+        if (p >= 0) {
+            float s[V];
+            const Pack<T, V> l = *reinterpret_cast<const Pack<T, V> *>(at_label + d);
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[i] = r * to_f(l.v[i]);
             for (int32_t k = 0; k < parts; ++k) {
                 const Pack<float, V> x = *reinterpret_cast<const Pack<float, V> *>(acc + ((int64_t)k * rows + p) * Dp + d);
 #pragma unroll
                 for (int i = 0; i < V; ++i) s[i] += x.v[i];
             }
 #pragma unroll
-        for (int i = 0; i < V; ++i) o.v[i] = from_f<T>(p >= 0 ? s[i] * f : 0.0f);
+            for (int i = 0; i < V; ++i) o.v[i] = from_f<T>(s[i] * f);
+        }
         *reinterpret_cast<Pack<T, V> *>(out + n * os + d) = o;
     }
 }
@@ -188,7 +186,7 @@ struct Plan {
     int32_t Dp, tiles_v, piece, pieces, vocab_blocks;   // piece: columns of the vocabulary that g holds at a time
     int64_t Lp, acc_rows;
     bool copy_weight;
-    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_factor, *hit; float2 *part; char *rows, *scaled, *weight, *grad; float *acc;
+    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_factor, *rest, *hit; float2 *part; char *rows, *weight, *grad; float *acc;
     size_t bytes;
 };
 
@@ -214,7 +212,7 @@ inline Plan make_plan(void *base, int64_t N, int64_t V, int64_t D, const void *w
     } else {
         p.row_lse = (float *)take(p.Lp * 4);
         p.row_factor = (float *)take(p.Lp * 4);
-        p.scaled = take((size_t)p.Lp * p.Dp * 2);
+        p.rest = (float *)take(p.Lp * 4);
         const int64_t most = kPieceBytes / (2 * p.Lp) / kTileM * kTileM, whole = ceil_div(V, kTileM) * kTileM;
         p.piece = (int32_t)(most < kTileM ? kTileM : most < whole ? most : whole);
         p.pieces = (int32_t)ceil_div(V, p.piece);
@@ -287,13 +285,12 @@ int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, 
     const int32_t pairs = pairs_on_device<T>();
     if (pairs == 0) return DC_ERR_CUDA;
     g.vocab_blocks = p.vocab_blocks; g.pairs = pairs; g.acc_rows = p.acc_rows;
-    if (!dw) g.scaled = nullptr;
     if (int e = gather<T>(g, st)) return e;
     readable<T>(p, g, &weight, &ws, st);
     const int ob = dw_f32 ? 4 : 2;
-    CUtensorMap rows, grad_k, grad_mn, scaled_mn;
+    CUtensorMap rows, rows_mn, grad_k, grad_mn;
     if (!tensor_map(&rows, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&grad_k, p.grad, bf, p.piece, p.Lp, p.piece, 128) ||
-        !tensor_map(&grad_mn, p.grad, bf, p.piece, p.Lp, p.piece, 64) || !tensor_map(&scaled_mn, p.scaled, bf, p.Dp, p.Lp, p.Dp, 64))
+        !tensor_map(&grad_mn, p.grad, bf, p.piece, p.Lp, p.piece, 64) || !tensor_map(&rows_mn, p.rows, bf, p.Dp, p.Lp, p.Dp, 64))
         return DC_ERR_CUDA;
     const int64_t tm = p.Lp / kTileM, td = ceil_div(g.D, kTileN);
     for (int32_t k = 0; k < p.pieces; ++k) {
@@ -302,7 +299,7 @@ int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, 
         CUtensorMap w_k, w_mn;
         if (!tensor_map(&w_k, w, bf, g.D, nv, ws, 128) || !tensor_map(&w_mn, w, bf, g.D, nv, ws, 64)) return DC_ERR_CUDA;
         Product q{};
-        q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.lse = p.row_lse; q.grad = p.grad; q.piece = p.piece;
+        q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.lse = p.row_lse; q.factor = p.row_factor; q.rest = p.rest; q.grad = p.grad; q.piece = p.piece;
         q.v0 = (int32_t)v0; q.V = (int32_t)nv; q.D = g.D; q.Dp = p.Dp; q.grad_scale = grad_scale<T>();
         if (int e = launch_units<T, kGrad>(tm * ceil_div(nv, kTileN), pairs, rows, w_k, rows, w_k, q, st)) return e;
         if (dw) {
@@ -312,13 +309,13 @@ int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, 
         q.acc = dh ? p.acc : nullptr;
         q.first = k == 0; q.vocab_blocks = p.vocab_blocks; q.grad_scale = 1.0f / grad_scale<T>();
         const int64_t units = (dw ? ceil_div(nv, kTileM) * td : 0) + (dh ? tm * td * kMaxParts : 0);
-        if (int e = launch_units<T, kBack>(units, pairs, grad_k, w_mn, grad_mn, scaled_mn, q, st)) return e;
+        if (int e = launch_units<T, kBack>(units, pairs, grad_k, w_mn, grad_mn, rows_mn, q, st)) return e;
     }
     if (!dh) return DC_OK;
     const unsigned blocks = (unsigned)ceil_div(g.N, 8);
     const float unscale = 1.0f / grad_scale<T>();
-    if (g.D % 4 == 0 && rows_on(dh, dhs, 2, 8)) vocab_put_back<T, 4><<<blocks, 256, 0, st>>>(p.head, p.pos_of, p.row_factor, p.acc, g.N, g.D, p.Dp, unscale, (T *)dh, dhs);
-    else vocab_put_back<T, 1><<<blocks, 256, 0, st>>>(p.head, p.pos_of, p.row_factor, p.acc, g.N, g.D, p.Dp, unscale, (T *)dh, dhs);
+    if (g.D % 4 == 0 && rows_on(dh, dhs, 2, 8) && rows_on(weight, ws, 2, 8)) vocab_put_back<T, 4><<<blocks, 256, 0, st>>>(p.head, p.pos_of, p.label, p.rest, p.acc, (const T *)weight, ws, g.N, g.D, p.Dp, unscale, (T *)dh, dhs);
+    else vocab_put_back<T, 1><<<blocks, 256, 0, st>>>(p.head, p.pos_of, p.label, p.rest, p.acc, (const T *)weight, ws, g.N, g.D, p.Dp, unscale, (T *)dh, dhs);
     return launched();
 }
 
@@ -375,7 +372,7 @@ extern "C" int dc_vocab_loss_backward(const void *hidden, int64_t hidden_stride,
     Gather g{};
     g.hidden = hidden; g.hs = hidden_stride; g.targets = targets; g.ignore = ignore_index; g.lse = lse; g.dloss = dloss; g.N = N; g.V = V;
     g.D = (int32_t)D; g.Dp = p.Dp; g.logit_scale = logit_scale; g.head = p.head; g.row_of = p.row_of; g.pos_of = p.pos_of; g.label = p.label;
-    g.row_lse = p.row_lse; g.row_factor = p.row_factor; g.rows = p.rows; g.scaled = p.scaled;
+    g.row_lse = p.row_lse; g.row_factor = p.row_factor; g.rows = p.rows;
     return dtype == DC_BF16
                ? backward<__nv_bfloat16>(g, p, weight, weight_stride, dhidden, dhidden_stride, dweight, dweight_stride, dweight_dtype == DC_F32, accumulate != 0, st)
                : backward<__half>(g, p, weight, weight_stride, dhidden, dhidden_stride, dweight, dweight_stride, dweight_dtype == DC_F32, accumulate != 0, st);
