@@ -45,7 +45,8 @@ int dc_embed(const void *table, int64_t table_stride, int32_t dtype, const int64
  *
  * The sum is taken in fp32 in a fixed order and rounded once to dtable_dtype, which is `dtype` or DC_F32.  Tokens that are
  * pad_id or outside [0, V) contribute nothing.  With accumulate = 0 every row of dtable is written; with accumulate = 1
- * only rows of tokens that occur are read and written.  N = 0 is allowed.  V <= DC_EMBED_MAX_V, N, D <= 2^30.
+ * only rows of tokens that occur are read and written (by additions in memory where dtable is fp32, which take subnormal
+ * numbers for zero).  N = 0 is allowed.  V <= DC_EMBED_MAX_V, N, D <= 2^30.
  *   workspace  at least dc_embed_backward_workspace_bytes(N, V, D) bytes, 256-byte aligned
  */
 #define DC_EMBED_MAX_V 4194304

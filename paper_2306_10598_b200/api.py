@@ -419,17 +419,22 @@ def _matrix(t: torch.Tensor, name: str, device: Optional[torch.device] = None, d
     """(pointer, row stride, rows, columns) of a tensor seen as a matrix."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dtype not in _DTYPE or (dtype is not None and t.dtype != dtype):
-        raise TypeError(f"{name} must be {dtype or 'bfloat16, float16 or float32'}, got {t.dtype}")
+    dt = t.dtype
+    if dt not in _DTYPE or (dtype is not None and dt != dtype):
+        raise TypeError(f"{name} must be {dtype or 'bfloat16, float16 or float32'}, got {dt}")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, not {device}")
-    if t.dim() < 1:
-        raise ValueError(f"{name} must have at least one dimension")
-    m = t if t.dim() == 2 else t.view(-1, t.shape[-1]) if t.numel() else t.reshape(0, t.shape[-1])
-    rows, cols = m.shape
-    if cols > 1 and rows > 0 and m.stride(1) != 1:
+    shape = t.shape
+    if len(shape) != 2:
+        if not shape:
+            raise ValueError(f"{name} must have at least one dimension")
+        t = t.view(-1, shape[-1]) if t.numel() else t.reshape(0, shape[-1])
+        shape = t.shape
+    rows, cols = shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1 and rows > 0:
         raise ValueError(f"the elements of a row of {name} must be adjacent")
-    return m.data_ptr(), (m.stride(0) if rows > 1 else max(1, cols)), rows, cols
+    return t.data_ptr(), (stride if rows > 1 else max(1, cols)), rows, cols
 
 
 def _vector(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, device: torch.device) -> int:
@@ -446,13 +451,19 @@ def _same(name: str, got, want) -> None:
         raise ValueError(f"{name} must be {tuple(want)}, got {tuple(got)}")
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream   # current_stream(device).cuda_stream without the Stream object (2 us a call)
+
+
 def _call(device: torch.device, where: str, fn, *args) -> None:
     """Calls `fn(*args, stream)` with `device` current."""
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream), where)
-        return
-    with torch.cuda.device(device):
-        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream), where)
+    index = device.index
+    if index == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, _raw_stream(index))
+    if status:
+        _check(status, where)
 
 
 def _workspace(ws: Optional[torch.Tensor], need: int, device: torch.device) -> torch.Tensor:
@@ -554,7 +565,7 @@ def dc_train_status() -> int:
 # The same with outputs and workspaces allocated by torch.
 
 def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, pad_id: int = -1) -> torch.Tensor:
-    out = torch.empty((*ids.shape, table.shape[-1]), dtype=table.dtype, device=table.device)
+    out = table.new_empty((*ids.shape, table.shape[-1]))
     dc_embed(table, ids, out, scale, pad_id)
     return out
 
@@ -582,17 +593,17 @@ class Saved8(NamedTuple):
 
 
 def gelu_save8(x: torch.Tensor) -> Saved8:
-    D = x.shape[-1]
-    r = Saved8(torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(x.shape, dtype=torch.int8, device=x.device),
-               torch.empty((*x.shape[:-1], -(-D // SAVE8_GROUP)), dtype=torch.float32, device=x.device))
+    shape = x.shape
+    r = Saved8(x.new_empty(shape), x.new_empty(shape, dtype=torch.int8),
+               x.new_empty((*shape[:-1], -(-shape[-1] // SAVE8_GROUP)), dtype=torch.float32))
     dc_gelu_save8(x, *r)
     return r
 
 
 def gelu_save8_backward(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, want_y: bool = False):
     """dx, or (dx, y_again) with want_y."""
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-    y = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device) if want_y else None
+    dx = dy.new_empty(dy.shape)
+    y = dy.new_empty(dy.shape) if want_y else None
     dc_gelu_save8_backward(dy, q, scales, dx, y)
     return (dx, y) if want_y else dx
 
@@ -604,8 +615,8 @@ class VocabLoss(NamedTuple):
 
 def vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100, logit_scale: float = 1.0,
                workspace: Optional[torch.Tensor] = None) -> VocabLoss:
-    loss = torch.empty(targets.shape, dtype=torch.float32, device=hidden.device)
-    lse = torch.empty(targets.shape, dtype=torch.float32, device=hidden.device)
+    loss = hidden.new_empty(targets.shape, dtype=torch.float32)
+    lse = hidden.new_empty(targets.shape, dtype=torch.float32)
     dc_vocab_loss(hidden, weight, targets, loss, lse,
                   _workspace(workspace, dc_vocab_loss_workspace_bytes(targets.numel(), weight, False), hidden.device), ignore_index, logit_scale)
     return VocabLoss(loss, lse)
@@ -618,9 +629,9 @@ def vocab_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
     """(dhidden, dweight): dweight is a new tensor of the weight's type, or the given one (that type or fp32) written or added to."""
     if accumulate and dweight is None:
         raise ValueError("accumulate needs the dweight to add to")
-    dh = torch.empty(hidden.shape, dtype=hidden.dtype, device=hidden.device) if want_dhidden else None
+    dh = hidden.new_empty(hidden.shape) if want_dhidden else None
     if dweight is None and want_dweight:
-        dweight = torch.empty(weight.shape, dtype=weight.dtype, device=weight.device)
+        dweight = weight.new_empty(weight.shape)
     dc_vocab_loss_backward(hidden, weight, targets, lse, dloss, dh, dweight,
                            _workspace(workspace, dc_vocab_loss_workspace_bytes(targets.numel(), weight, True), hidden.device),
                            ignore_index, logit_scale, accumulate)

@@ -12,7 +12,7 @@ constexpr int kTile = 32;            // places of the grouped list per tile
 constexpr int kBuckets = 128;        // blocks of embed_sort; more where a bucket would hold more than kMaxKeys tokens
 constexpr int kMaxKeys = 4096;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr int kList = 2048;          // places of a bucket that are put in order at a time
+constexpr int kWarpList = 128, kList = kSortWarps * kWarpList;   // places of a bucket that are put in order at a time
 
 // ---- lookup: a warp takes (row, chunk of columns), four packs to a lane ------------------------------------------------
 
@@ -54,13 +54,17 @@ __global__ void __launch_bounds__(256) embed_kernel(const T *__restrict__ table,
 // ---- grouping the places by token ----------------------------------------------------------------------------------------
 
 // Block b collects the places of tokens with token mod buckets = b, in order of place, and writes them token by token.
-// Every block reads all ids (from L2), so it also counts what goes before its own part: no block waits for another.
+// Every block reads all ids (from L2, eight loads of a thread in flight), so it also counts what goes before its own part and
+// no block waits for another.  16384 ids of 32768 tokens: see the figures at embed_sum.
 __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__restrict__ ids, int32_t N, int64_t vocab, int64_t pad, int32_t log_buckets,
-                                                           int32_t *__restrict__ place, int32_t *__restrict__ token, int32_t *__restrict__ live)
+                                                           int32_t *__restrict__ place, int32_t *__restrict__ token, int32_t *__restrict__ live,
+                                                           uint8_t *__restrict__ occurs)
 {
+    constexpr int U = 8;
     extern __shared__ int32_t hist[];                      // [keys]: how often each token of the bucket occurs, then where it goes
-    __shared__ int32_t list_place[kList], list_key[kList];
-    __shared__ int32_t warp_mine[kSortWarps], warp_less[kSortWarps];
+    __shared__ int32_t list_place[kList];
+    __shared__ uint16_t list_key[kList];
+    __shared__ int32_t warp_mine[kSortWarps], warp_less[kSortWarps], warp_sum[kSortWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t bucket = blockIdx.x, mask = gridDim.x - 1;
     const int32_t keys = (int32_t)((vocab + mask) >> log_buckets);
@@ -70,17 +74,31 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
     const int32_t seg = (N + kSortThreads - 1) / kSortThreads * 32;              // places of a warp, in order
     const int64_t lo = (int64_t)warp * seg, hi = lo + seg < N ? lo + seg : N;
     int32_t mine = 0, less = 0;
-    for (int64_t i = lo + lane; i < hi; i += 32) {
-        const int64_t id = ids[i];
-        const bool ok = id >= 0 && id < vocab && id != pad;
-        const int32_t b = (int32_t)id & mask;
-        if (ok && b == bucket) { ++mine; atomicAdd(&hist[id >> log_buckets], 1); }
-        less += ok && b < bucket;
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * U) {
+        int64_t id[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) id[u] = i0 + u * 32 + lane < hi ? ids[i0 + u * 32 + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool ok = id[u] >= 0 && id[u] < vocab && id[u] != pad;
+            const int32_t b = (int32_t)id[u] & mask;
+            const bool is = ok && b == bucket;
+            const uint32_t all = __ballot_sync(~0u, is);
+            const int32_t s = mine + __popc(all & ((1u << lane) - 1));
+            if (is) {
+                atomicAdd(&hist[id[u] >> log_buckets], 1);
+                if (s < kWarpList) {                                              // kept at once, as long as each warp has room
+                    list_place[warp * kWarpList + s] = (int32_t)(i0 + u * 32 + lane);
+                    list_key[warp * kWarpList + s] = (uint16_t)(id[u] >> log_buckets);
+                }
+            }
+            mine += __popc(all);
+            less += ok && b < bucket;
+        }
     }
-    mine = __reduce_add_sync(~0u, mine);
     less = __reduce_add_sync(~0u, less);
     if (lane == 0) { warp_mine[warp] = mine; warp_less[warp] = less; }
-    __syncthreads();
+    const bool kept = !__syncthreads_or(mine > kWarpList);
     int32_t begin = 0, total = 0, first = 0;                                      // of this warp, of the bucket, of the bucket's part
     for (int w = 0; w < kSortWarps; ++w) {
         if (w == warp) begin = total;
@@ -90,7 +108,6 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
     if (bucket == mask && tid == 0) *live = first + total;
 
     // exclusive sum over the tokens of the bucket: each thread a run of neighbours, then the warps' totals
-    __shared__ int32_t warp_sum[kSortWarps];
     const int32_t run = (keys + kSortThreads - 1) / kSortThreads, k0 = tid * run, k1 = min(keys, k0 + run);
     int32_t own = 0;
     for (int32_t k = k0; k < k1; ++k) own += hist[k];
@@ -103,10 +120,59 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
     __syncthreads();
     int32_t at = upto - own;
     for (int w = 0; w < warp; ++w) at += warp_sum[w];
-    for (int32_t k = k0; k < k1; ++k) { const int32_t c = hist[k]; hist[k] = at; at += c; }
+    for (int32_t k = k0; k < k1; ++k) {
+        const int32_t c = hist[k];
+        hist[k] = at;
+        at += c;
+        const int64_t v = ((int64_t)k << log_buckets) + bucket;
+        if (occurs && v < vocab) occurs[v] = c > 0;
+    }
+    __syncthreads();
 
-    for (int32_t from = 0; from < total; from += kList) {
+    // The places list_*[from_list ...] go where their token's next place is; a warp does 32 at a time.
+    auto put = [&](int32_t from_list, int32_t have) {
+        for (int32_t j0 = 0; j0 < have; j0 += 32) {
+            const bool is = j0 + lane < have;
+            const int32_t key = is ? list_key[from_list + j0 + lane] : -1;
+            const uint32_t same = __match_any_sync(~0u, key);
+            const int32_t rank = __popc(same & ((1u << lane) - 1));
+            const int32_t next = is ? hist[key] : 0;
+            __syncwarp();
+            if (is) {
+                if (rank == 0) hist[key] = next + __popc(same);
+                place[first + next + rank] = list_place[from_list + j0 + lane];
+                token[first + next + rank] = (key << log_buckets) + bucket;
+            }
+            __syncwarp();
+        }
+    };
+    // one warp after the other
+    auto put_in_turn = [&](int32_t have) {
+        for (int w = 0; w < kSortWarps; ++w) {
+            if (w == warp) put(warp * kWarpList, have);
+            __syncthreads();
+        }
+    };
+    if (kept && total <= 1024) {
+        // few: they move together first, and one warp puts them, without 32 turns
+        int32_t p[kWarpList / 32], k[kWarpList / 32];
+#pragma unroll
+        for (int i = 0; i < kWarpList / 32; ++i)
+            if (i * 32 + lane < mine) { p[i] = list_place[warp * kWarpList + i * 32 + lane]; k[i] = list_key[warp * kWarpList + i * 32 + lane]; }
         __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kWarpList / 32; ++i)
+            if (i * 32 + lane < mine) { list_place[begin + i * 32 + lane] = p[i]; list_key[begin + i * 32 + lane] = (uint16_t)k[i]; }
+        __syncthreads();
+        if (warp == 0) put(0, total);
+        return;
+    }
+    if (kept) {
+        put_in_turn(mine);
+        return;
+    }
+    // more places than a warp has room for (a token that holds a large part of many): the ids again, kList places at a time
+    for (int32_t from = 0; from < total; from += kList) {
         int32_t r = begin;
         if (begin < from + kList && begin + mine > from)
             for (int64_t i0 = lo; i0 < hi; i0 += 32) {
@@ -115,35 +181,34 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
                 const bool is = id >= 0 && id < vocab && id != pad && ((int32_t)id & mask) == bucket;
                 const uint32_t all = __ballot_sync(~0u, is);
                 const int32_t s = r + __popc(all & ((1u << lane) - 1)) - from;
-                if (is && s >= 0 && s < kList) { list_place[s] = (int32_t)i; list_key[s] = (int32_t)(id >> log_buckets); }
+                if (is && s >= 0 && s < kList) { list_place[s] = (int32_t)i; list_key[s] = (uint16_t)(id >> log_buckets); }
                 r += __popc(all);
             }
         __syncthreads();
-        if (warp == 0) {
-            const int32_t m = min(kList, total - from);
-            for (int32_t j0 = 0; j0 < m; j0 += 32) {
-                const int32_t j = j0 + lane;
-                const int32_t key = j < m ? list_key[j] : -1;
-                const uint32_t same = __match_any_sync(~0u, key);
-                const int32_t rank = __popc(same & ((1u << lane) - 1));
-                int32_t to = j < m ? hist[key] : 0;
-                __syncwarp();
-                if (j < m) {
-                    if (rank == 0) hist[key] = to + __popc(same);
-                    to += first + rank;
-                    place[to] = list_place[j];
-                    token[to] = (key << log_buckets) + bucket;
-                }
-                __syncwarp();
-            }
-        }
+        put_in_turn(max(0, min(kWarpList, total - from - warp * kWarpList)));
     }
 }
 
 // ---- sums over the grouped list -------------------------------------------------------------------------------------------
 
+// Each element of dtable is met once in a call.  In fp32 the addition is left to memory (red): the warp does not wait for the
+// old value, which a run of rare tokens would otherwise do place after place.
 template <class O, int V> __device__ __forceinline__ void finish_row(O *row, const float (&sum)[V], float scale, bool accumulate)
 {
+    if constexpr (sizeof(O) == 4) {
+        if (accumulate) {
+            if constexpr (V >= 4) {
+#pragma unroll
+                for (int i = 0; i < V; i += 4)
+                    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(row + i), "f"(scale * sum[i]), "f"(scale * sum[i + 1]),
+                                 "f"(scale * sum[i + 2]), "f"(scale * sum[i + 3]) : "memory");
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) asm volatile("red.global.add.f32 [%0], %1;" ::"l"(row + i), "f"(scale * sum[i]) : "memory");
+            }
+            return;
+        }
+    }
     Pack<O, V> o;
     if (accumulate) o = *reinterpret_cast<const Pack<O, V> *>(row);
 #pragma unroll
@@ -156,10 +221,21 @@ template <class O, int V> __device__ __forceinline__ void finish_row(O *row, con
 template <class T, class O, int V>
 __global__ void __launch_bounds__(128) embed_sum(const T *__restrict__ dout, int64_t ds, const int32_t *__restrict__ place, const int32_t *__restrict__ token,
                                                  const int32_t *__restrict__ live, int64_t D, float scale, O *__restrict__ dtable, int64_t ts, bool accumulate,
-                                                 float *__restrict__ part, int64_t pitch, int32_t chunks)
+                                                 float *__restrict__ part, int64_t pitch, int32_t chunks, int64_t sum_blocks, const uint8_t *__restrict__ occurs,
+                                                 int64_t vocab)
 {
     constexpr int U = 8;                                   // rows on their way at a time
     const int lane = threadIdx.x & 31;
+    if (blockIdx.x >= sum_blocks) {
+        // rows of tokens that do not occur
+        const int64_t step = (int64_t)(gridDim.x - sum_blocks) * 4;
+        for (int64_t v = (blockIdx.x - sum_blocks) * 4 + (threadIdx.x >> 5); v < vocab; v += step) {
+            if (occurs[v]) continue;
+            const Pack<O, V> zero = {};
+            for (int64_t c = lane * V; c < D; c += 32 * V) *reinterpret_cast<Pack<O, V> *>(dtable + v * ts + c) = zero;
+        }
+        return;
+    }
     const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     const int64_t tile = task / chunks;
     const int64_t c = (task - tile * chunks) * (32 * V) + lane * V;
@@ -209,30 +285,59 @@ __global__ void __launch_bounds__(128) embed_sum(const T *__restrict__ dout, int
     }
 }
 
-// A token that begins in a tile and goes on in the next: its partial sums in the order of the tiles.
+// A token that begins in a tile and goes on in the next: its partial sums in the order of the tiles, a quarter of them to each
+// warp of the block.
 template <class O, int V>
 __global__ void __launch_bounds__(128) embed_join(const int32_t *__restrict__ token, const int32_t *__restrict__ live, int64_t D, float scale,
-                                                  O *__restrict__ dtable, int64_t ts, bool accumulate, const float *__restrict__ part, int64_t pitch,
-                                                  int32_t chunks)
+                                                  O *__restrict__ dtable, int64_t ts, bool accumulate, const float *__restrict__ part, int64_t pitch)
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int64_t tile = task / chunks;
-    const int64_t c = (task - tile * chunks) * (32 * V) + lane * V;
+    constexpr int U = 8;
+    __shared__ float quarter[4][V][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t tile = blockIdx.x;
     const int32_t n = *live;
     const int64_t end = (tile + 1) * kTile;
     if (end >= n) return;                                                    // the last tile has nothing behind it
     const int32_t tok = token[end - 1];
     if (token[end] != tok) return;                                           // nothing goes on
     if (tile > 0 && token[tile * kTile] == tok && token[tile * kTile - 1] == tok) return;   // it began in an earlier tile
-    if (c >= D) return;
-    float sum[V];
+    int64_t last = tile + 1;                                                 // the tile that it ends in
+    for (;;) {
+        const int64_t t = last + 1 + lane;
+        const uint32_t on = __ballot_sync(~0u, t * kTile < n && token[min(t * kTile, (int64_t)n - 1)] == tok);
+        last += on == ~0u ? 32 : __ffs(~on) - 1;
+        if (on != ~0u) break;
+    }
+    const int64_t each = (last - tile + 3) / 4, t0 = tile + 1 + warp * each, t1 = min(last + 1, t0 + each);
+    const int64_t c = (int64_t)blockIdx.y * (32 * V) + lane * V;
+    float sum[V] = {};
+    if (c < D) {
+        if (warp == 0) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum[i] = part[(tile * 2 + 1) * pitch + c + i];
-    for (int64_t t = tile + 1; t * kTile < n && token[t * kTile] == tok; ++t)
+            for (int i = 0; i < V; ++i) sum[i] = part[(tile * 2 + 1) * pitch + c + i];
+        }
+        for (int64_t t = t0; t < t1; t += U) {
+            float x[U][V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[i] += part[t * 2 * pitch + c + i];
-    finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[u][i] = t + u < t1 ? part[(t + u) * 2 * pitch + c + i] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] += x[u][i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) quarter[warp][i][lane] = sum[i];
+    __syncthreads();
+    if (warp == 0 && c < D) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w)
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] += quarter[w][i][lane];
+        finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
+    }
 }
 
 struct SortPlan { int32_t log_buckets; int32_t keys; };
@@ -245,8 +350,8 @@ inline SortPlan sort_plan(int64_t V)
     return p;
 }
 
-struct Work { int32_t *live, *place, *token; float *part; int64_t pitch; size_t bytes; };
-inline Work carve(void *base, int64_t N, int64_t D)
+struct Work { int32_t *live, *place, *token; uint8_t *occurs; float *part; int64_t pitch; size_t bytes; };
+inline Work carve(void *base, int64_t N, int64_t vocab, int64_t D)
 {
     Work w{};
     char *p = (char *)base;
@@ -256,6 +361,8 @@ inline Work carve(void *base, int64_t N, int64_t D)
     at += align_up((size_t)N * 4, 256);
     w.token = (int32_t *)(p + at);
     at += align_up((size_t)N * 4, 256);
+    w.occurs = (uint8_t *)(p + at);
+    at += align_up((size_t)vocab, 256);
     w.part = (float *)(p + at);
     w.pitch = ceil_div(D, 8) * 8;
     at += align_up((size_t)ceil_div(N, kTile) * 2 * (size_t)w.pitch * 4, 256);
@@ -264,13 +371,17 @@ inline Work carve(void *base, int64_t N, int64_t D)
 }
 
 template <class T, class O, int V>
-int backward_launch(const void *dout, int64_t ds, int64_t N, int64_t D, float scale, void *dtable, int64_t ts, bool accumulate, const Work &w, cudaStream_t st)
+int backward_launch(const void *dout, int64_t ds, int64_t N, int64_t vocab, int64_t D, float scale, void *dtable, int64_t ts, bool accumulate, const Work &w,
+                    cudaStream_t st)
 {
     const int32_t chunks = (int32_t)ceil_div(D, 32 * V);
-    const int64_t blocks = ceil_div(ceil_div(N, kTile) * chunks, 4);
-    if (blocks > INT32_MAX) return DC_ERR_RANGE;
-    embed_sum<T, O, V><<<(unsigned)blocks, 128, 0, st>>>((const T *)dout, ds, w.place, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch, chunks);
-    embed_join<O, V><<<(unsigned)blocks, 128, 0, st>>>(w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch, chunks);
+    const int64_t tiles = ceil_div(N, kTile), sums = ceil_div(tiles * chunks, 4);
+    int64_t zeros = accumulate ? 0 : ceil_div(vocab, 4);
+    if (zeros > (int64_t)sm_count() * 16) zeros = (int64_t)sm_count() * 16;
+    if (sums + zeros > INT32_MAX || chunks > 65535) return DC_ERR_RANGE;
+    embed_sum<T, O, V><<<(unsigned)(sums + zeros), 128, 0, st>>>((const T *)dout, ds, w.place, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part,
+                                                                 w.pitch, chunks, sums, w.occurs, vocab);
+    embed_join<O, V><<<dim3((unsigned)tiles, (unsigned)chunks), 128, 0, st>>>(w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch);
     return launched();
 }
 
@@ -318,7 +429,7 @@ extern "C" int dc_embed(const void *table, int64_t table_stride, int32_t dtype, 
 extern "C" size_t dc_embed_backward_workspace_bytes(int64_t N, int64_t V, int64_t D)
 {
     if (N < 0 || V <= 0 || D <= 0 || N > kMaxDim || V > DC_EMBED_MAX_V || D > kMaxDim) return 0;
-    return carve(nullptr, N, D).bytes;
+    return carve(nullptr, N, V, D).bytes;
 }
 
 extern "C" int dc_embed_backward(const void *dout, int64_t dout_stride, int32_t dtype, const int64_t *ids, int64_t N, int64_t V, int64_t D, float scale,
@@ -333,17 +444,20 @@ extern "C" int dc_embed_backward(const void *dout, int64_t dout_stride, int32_t 
     const int eb = elem_bytes(dtype), ob = elem_bytes(dtable_dtype);
     if (!on(dtable, ob) || (N > 0 && (!on(dout, eb) || !on(ids, 8)))) return DC_ERR_ALIGN;
     const cudaStream_t st = (cudaStream_t)stream;
-    if (N > 0 && (!workspace || !on(workspace, 256) || workspace_bytes < carve(nullptr, N, D).bytes)) return DC_ERR_WORKSPACE;
-    if (!accumulate && cudaMemset2DAsync(dtable, (size_t)dtable_stride * ob, 0, (size_t)D * ob, (size_t)V, st) != cudaSuccess) return DC_ERR_CUDA;
-    if (N == 0) return DC_OK;
-    const Work w = carve(workspace, N, D);
+    if (N > 0 && (!workspace || !on(workspace, 256) || workspace_bytes < carve(nullptr, N, V, D).bytes)) return DC_ERR_WORKSPACE;
+    if (N == 0) {
+        if (accumulate) return DC_OK;
+        return cudaMemset2DAsync(dtable, (size_t)dtable_stride * ob, 0, (size_t)D * ob, (size_t)V, st) == cudaSuccess ? DC_OK : DC_ERR_CUDA;
+    }
+    if (sm_count() == 0) return DC_ERR_CUDA;
+    const Work w = carve(workspace, N, V, D);
     const SortPlan p = sort_plan(V);
     if (pad_id < 0) pad_id = INT64_MIN;
-    embed_sort<<<1u << p.log_buckets, kSortThreads, (size_t)p.keys * 4, st>>>(ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token, w.live);
+    embed_sort<<<1u << p.log_buckets, kSortThreads, (size_t)p.keys * 4, st>>>(ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token, w.live, accumulate ? nullptr : w.occurs);
     // packs of V elements on both sides: 16 bytes of dout, and as many elements of dtable
     const int W = 16 / eb;
     const bool wide = D % W == 0 && rows_on(dout, dout_stride, eb, 16) && rows_on(dtable, dtable_stride, ob, (size_t)(W * ob));
-#define DCT_SUM(T, O, V_) backward_launch<T, O, V_>(dout, dout_stride, N, D, scale, dtable, dtable_stride, accumulate != 0, w, st)
+#define DCT_SUM(T, O, V_) backward_launch<T, O, V_>(dout, dout_stride, N, V, D, scale, dtable, dtable_stride, accumulate != 0, w, st)
     if (dtype == DC_F32) return wide ? DCT_SUM(float, float, 4) : DCT_SUM(float, float, 1);
     if (dtype == DC_BF16) {
         if (dtable_dtype == DC_F32) return wide ? DCT_SUM(__nv_bfloat16, float, 8) : DCT_SUM(__nv_bfloat16, float, 1);

@@ -1,141 +1,220 @@
 // dc_gelu_save8 and its backward pass: gelu with x kept as 8-bit integers and one scale per 128 neighbours of a row.
 //
-// Both kernels touch every element once (16-bit types: forward 2 bytes in, 2 + 1 out; backward 2 + 1 in, 2 + 2 out) and do
-// about 30 operations on it, so memory bounds them.  A group of 128 is held by 128/V lanes with V adjacent elements each
-// (V = 16 bytes' worth), which makes its maximum a few shuffles and leaves nothing to pass through shared memory.
+// Both kernels touch every element once (16-bit types: forward 2 bytes in, 2 + 1 out; backward 2 + 1 in, 2 + 2 out), so memory
+// bounds them as long as an element costs less than about 25 instructions, 3 of them on the special-function unit.  A group of
+// 128 is held by 128/V lanes with V adjacent elements each (V = 16 bytes' worth), which makes its maximum a few shuffles and
+// leaves nothing to pass through shared memory; a thread has kAhead groups on their way at once.  Conversions between integers
+// and floats, which would go to the special-function unit too, are done by adding a constant whose last bits are the integer.
 #include "train_common.cuh"
 
 namespace dct {
 
 constexpr int kGroup = DC_SAVE8_GROUP;
-constexpr float kTwoA = 1.5957691216057308f;   // 2 sqrt(2/pi)
-constexpr float kB = 0.044715f;
 constexpr int kThreads = 256;
+constexpr int kAhead = 4;
+constexpr float kTwoA = 1.5957691216057308f;                   // 2 sqrt(2/pi)
+constexpr float kB = 0.044715f;
+constexpr float kLog2E = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 // sigma(2u), u = sqrt(2/pi)(v + B v^3), so that gelu(v) = v gate(v).  exp overflows to +inf for very negative v, which
 // gives the gate 0.
 __device__ __forceinline__ float gate(float v)
 {
-    return __fdividef(1.0f, 1.0f + __expf(-kTwoA * (v + kB * v * v * v)));
+    return reciprocal(1.0f + exp2_fast(v * fmaf(-kTwoA * kB * kLog2E, v * v, -kTwoA * kLog2E)));
 }
 
-// How the lanes of a warp hold a group: packs of V elements, LPG lanes to a group, K packs to a lane.
+// V whole numbers of 8 bits, four to a word where there are as many.
+template <int V> struct alignas(V) Bytes { uint32_t w[V / 4]; };
+template <> struct alignas(1) Bytes<1> { uint8_t w[1]; };
+// number i as a float: 2^23 + (q + 128) as bits, less 2^23 + 128
+template <int V> __device__ __forceinline__ float whole(const Bytes<V> &b, int i)
+{
+    return __uint_as_float(__byte_perm(b.w[i / 4] ^ 0x80808080u, 0x4b000000u, 0x7440 | (i & 3))) - 8388736.0f;
+}
+__device__ __forceinline__ float whole(const Bytes<1> &b, int) { return __uint_as_float(0x4b000000u | (b.w[0] ^ 0x80u)) - 8388736.0f; }
+// the nearest whole number to r, ties to even, in the last byte: 1.5 2^23 + r is rounded to whole numbers
+__device__ __forceinline__ uint32_t nearest(float r) { return __float_as_uint(__fadd_rn(r, 12582912.0f)); }
+template <int V> __device__ __forceinline__ Bytes<V> bytes_of(const uint32_t (&n)[V])
+{
+    Bytes<V> b;
+#pragma unroll
+    for (int i = 0; i < V; i += 4) b.w[i / 4] = __byte_perm(__byte_perm(n[i], n[i + 1], 0x0040), __byte_perm(n[i + 2], n[i + 3], 0x0040), 0x5410);
+    return b;
+}
+template <> __device__ __forceinline__ Bytes<1> bytes_of<1>(const uint32_t (&n)[1]) { return Bytes<1>{{(uint8_t)n[0]}}; }
+
+// The largest magnitude of a pack, kept in the type's own pairs; a NaN stays.
+template <class T> struct Top;
+template <> struct Top<__nv_bfloat16> {
+    __nv_bfloat162 m = __nv_bfloat162(__float2bfloat16(0.0f), __float2bfloat16(0.0f));
+    __device__ void add(__nv_bfloat16 a, __nv_bfloat16 b) { m = __hmax2_nan(m, __habs2(__nv_bfloat162(a, b))); }
+    __device__ void swap(int d) { m = __hmax2_nan(m, __shfl_xor_sync(~0u, m, d)); }
+    __device__ float value() const { return __bfloat162float(__hmax_nan(m.x, m.y)); }
+};
+template <> struct Top<__half> {
+    __half2 m = __half2(__float2half(0.0f), __float2half(0.0f));
+    __device__ void add(__half a, __half b) { m = __hmax2_nan(m, __habs2(__half2(a, b))); }
+    __device__ void swap(int d) { m = __hmax2_nan(m, __shfl_xor_sync(~0u, m, d)); }
+    __device__ float value() const { return __half2float(__hmax_nan(m.x, m.y)); }
+};
+template <> struct Top<float> {
+    uint32_t m = 0;                                            // the bits of non-negative floats keep their order; NaN is on top
+    __device__ void add(float a, float b) { m = max(m, max(__float_as_uint(fabsf(a)), __float_as_uint(fabsf(b)))); }
+    __device__ void swap(int d) { m = max(m, __shfl_xor_sync(~0u, m, d)); }
+    __device__ float value() const { return __uint_as_float(m); }
+};
+
+// How the lanes of a warp hold a group: packs of V elements, LPG lanes to a group, K packs to a lane.  A block has PER groups on
+// their way, a thread every GAP-th of them.
 template <class T, int V> struct Hold {
     static constexpr int LPG = kGroup / V < 32 ? kGroup / V : 32;
     static constexpr int K = kGroup / (V * LPG);
+    static constexpr int GAP = kThreads / LPG, PER = GAP * kAhead;
 };
 
-// The groups a thread works on: first, then every `step`-th, as (row, group of the row) without a division per group.
-struct GroupWalk {
-    int64_t row, drow, left;
-    int32_t g, dg, per_row;
-    __device__ GroupWalk(int64_t first, int64_t step, int64_t total, int32_t per_row_) : per_row(per_row_)
+// Where the groups of a thread are, as (row, first column).  FLAT: the matrix is one row of whole groups.
+template <bool FLAT> struct Groups {
+    int64_t row, col, drow, dcol, D, wrap;
+    __device__ Groups(int64_t first, int64_t gap, int64_t per_row, int64_t D_) : D(D_)
     {
-        row = first / per_row;
-        g = (int32_t)(first - row * per_row);
-        drow = step / per_row;
-        dg = (int32_t)(step - drow * per_row);
-        left = first < total ? (total - first + step - 1) / step : 0;
+        if (FLAT) {
+            row = 0;
+            col = first * kGroup;
+            dcol = gap * kGroup;
+            return;
+        }
+        row = first / per_row;                                 // the only divisions of a thread
+        col = (first - row * per_row) * kGroup;
+        drow = gap / per_row;
+        dcol = (gap - drow * per_row) * kGroup;
+        wrap = per_row * kGroup;
     }
     __device__ __forceinline__ void next()
     {
-        --left;
+        col += dcol;
+        if (FLAT) return;
         row += drow;
-        g += dg;
-        if (g >= per_row) { g -= per_row; ++row; }
+        if (col >= D) { col -= wrap; ++row; }
     }
 };
 
-template <class T, int V>
-__global__ void __launch_bounds__(kThreads) gelu_save8_kernel(const T *__restrict__ x, int64_t xs, int64_t N, int32_t D, T *__restrict__ y, int64_t ys,
+template <class T, int V, bool FLAT>
+__global__ void __launch_bounds__(kThreads) gelu_save8_kernel(const T *__restrict__ x, int64_t xs, int64_t N, int64_t D, T *__restrict__ y, int64_t ys,
                                                               int8_t *__restrict__ q, float *__restrict__ scales)
 {
     using H = Hold<T, V>;
     const int lane = threadIdx.x % H::LPG;
-    const int32_t per_row = (D + kGroup - 1) / kGroup;
-    const int64_t total = N * per_row, step = (int64_t)gridDim.x * (kThreads / H::LPG);
-    GroupWalk w((int64_t)blockIdx.x * (kThreads / H::LPG) + threadIdx.x / H::LPG, step, total, per_row);
-    // the lanes of a warp stay together: all go on while one of them has a group left
-    while (__any_sync(~0u, w.left > 0)) {
-        float v[H::K][V];
-        uint32_t top = 0;
+    const int64_t per_row = (D + kGroup - 1) / kGroup, first = (int64_t)blockIdx.x * H::PER + threadIdx.x / H::LPG;
+    Groups<FLAT> g(first, H::GAP, per_row, D);
+    Pack<T, V> p[kAhead][H::K];
+    int64_t row[kAhead], col[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        row[u] = g.row;
+        col[u] = g.col;
 #pragma unroll
         for (int k = 0; k < H::K; ++k) {
-            const int32_t c = w.g * kGroup + (k * H::LPG + lane) * V;
-            Pack<T, V> p = {};
-            if (w.left > 0 && c < D) p = *reinterpret_cast<const Pack<T, V> *>(x + w.row * xs + c);
+            const int64_t c = col[u] + (k * H::LPG + lane) * V;
+            p[u][k] = Pack<T, V>{};
+            if (row[u] < N && c < D) p[u][k] = *reinterpret_cast<const Pack<T, V> *>(x + row[u] * xs + c);
+        }
+        g.next();
+    }
+    Top<T> top[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+        for (int k = 0; k < H::K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; i += 2) top[u].add(p[u][k].v[i], p[u][k].v[V > 1 ? i + 1 : i]);
+#pragma unroll
+        for (int d = H::LPG / 2; d; d >>= 1) top[u].swap(d);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const float a = top[u].value();
+        const bool finite = a < INFINITY, live = a > 0x1p-100f && finite;
+        const float inv = live ? __fdiv_rn(127.0f, a) : 0.0f;
+        if (row[u] >= N) continue;
+        if (lane == 0) scales[row[u] * per_row + col[u] / kGroup] = live ? __fmul_rn(a, 1.0f / 127.0f) : finite ? 0.0f : __uint_as_float(0x7fffffffu);
+#pragma unroll
+        for (int k = 0; k < H::K; ++k) {
+            const int64_t c = col[u] + (k * H::LPG + lane) * V;
+            if (c >= D) continue;
+            Pack<T, V> o;
+            uint32_t n[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                v[k][i] = to_f(p.v[i]);
-                top = max(top, __float_as_uint(fabsf(v[k][i])));   // the bits of non-negative floats keep their order; NaN is on top
+                const float v = to_f(p[u][k].v[i]);
+                o.v[i] = from_f<T>(v * gate(v));
+                n[i] = nearest(live ? __fmul_rn(v, inv) : 0.0f);
             }
+            *reinterpret_cast<Pack<T, V> *>(y + row[u] * ys + c) = o;
+            *reinterpret_cast<Bytes<V> *>(q + row[u] * D + c) = bytes_of<V>(n);
         }
-#pragma unroll
-        for (int m = H::LPG / 2; m; m >>= 1) top = max(top, __shfl_xor_sync(~0u, top, m));
-        const float a = __uint_as_float(top);
-        const bool finite = top < 0x7f800000u;
-        const bool live = a > 0x1p-100f && finite;
-        const float inv = live ? __fdiv_rn(127.0f, a) : 0.0f;
-        const float scale = live ? __fmul_rn(a, 1.0f / 127.0f) : finite ? 0.0f : __uint_as_float(0x7fffffffu);
-        if (w.left > 0) {
-            if (lane == 0) scales[w.row * per_row + w.g] = scale;
-#pragma unroll
-            for (int k = 0; k < H::K; ++k) {
-                const int32_t c = w.g * kGroup + (k * H::LPG + lane) * V;
-                if (c >= D) continue;
-                Pack<T, V> o;
-                Pack<int8_t, V> b;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    o.v[i] = from_f<T>(v[k][i] * gate(v[k][i]));
-                    b.v[i] = live ? (int8_t)__float2int_rn(__fmul_rn(v[k][i], inv)) : (int8_t)0;
-                }
-                *reinterpret_cast<Pack<T, V> *>(y + w.row * ys + c) = o;
-                *reinterpret_cast<Pack<int8_t, V> *>(q + w.row * D + c) = b;
-            }
-        }
-        if (w.left > 0) w.next();
     }
 }
 
-template <class T, int V>
+template <class T, int V, bool FLAT>
 __global__ void __launch_bounds__(kThreads) gelu_save8_backward_kernel(const T *__restrict__ dy, int64_t dys, const int8_t *__restrict__ q,
-                                                                       const float *__restrict__ scales, int64_t N, int32_t D, T *__restrict__ dx,
+                                                                       const float *__restrict__ scales, int64_t N, int64_t D, T *__restrict__ dx,
                                                                        int64_t dxs, T *__restrict__ y, int64_t ys)
 {
     using H = Hold<T, V>;
     const int lane = threadIdx.x % H::LPG;
-    const int32_t per_row = (D + kGroup - 1) / kGroup;
-    const int64_t total = N * per_row, step = (int64_t)gridDim.x * (kThreads / H::LPG);
-    for (GroupWalk w((int64_t)blockIdx.x * (kThreads / H::LPG) + threadIdx.x / H::LPG, step, total, per_row); w.left > 0; w.next()) {
-        const float scale = scales[w.row * per_row + w.g];
+    const int64_t per_row = (D + kGroup - 1) / kGroup, first = (int64_t)blockIdx.x * H::PER + threadIdx.x / H::LPG;
+    Groups<FLAT> g(first, H::GAP, per_row, D);
+    Pack<T, V> p[kAhead][H::K];
+    Bytes<V> b[kAhead][H::K];
+    float scale[kAhead];
+    int64_t row[kAhead], col[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        row[u] = g.row;
+        col[u] = g.col;
+        if (row[u] < N) scale[u] = scales[row[u] * per_row + col[u] / kGroup];
 #pragma unroll
         for (int k = 0; k < H::K; ++k) {
-            const int32_t c = w.g * kGroup + (k * H::LPG + lane) * V;
-            if (c >= D) continue;
-            const Pack<T, V> d = *reinterpret_cast<const Pack<T, V> *>(dy + w.row * dys + c);
-            const Pack<int8_t, V> b = *reinterpret_cast<const Pack<int8_t, V> *>(q + w.row * D + c);
+            const int64_t c = col[u] + (k * H::LPG + lane) * V;
+            if (row[u] < N && c < D) {
+                p[u][k] = *reinterpret_cast<const Pack<T, V> *>(dy + row[u] * dys + c);
+                b[u][k] = *reinterpret_cast<const Bytes<V> *>(q + row[u] * D + c);
+            }
+        }
+        g.next();
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+        for (int k = 0; k < H::K; ++k) {
+            const int64_t c = col[u] + (k * H::LPG + lane) * V;
+            if (row[u] >= N || c >= D) continue;
             Pack<T, V> o, r;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float v = (float)b.v[i] * scale, s = gate(v);
+                const float v = whole(b[u][k], i) * scale[u], s = gate(v);
                 const float near = fminf(fmaxf(v, -64.0f), 64.0f);   // beyond, s (1 - s) is 0 and v^2 must not make it NaN
-                const float slope = s + near * s * (1.0f - s) * (kTwoA + 3.0f * kB * kTwoA * near * near);
-                o.v[i] = from_f<T>(to_f(d.v[i]) * (isnan(v) ? v : slope));
+                const float slope = fmaf(near * fmaf(3.0f * kB * kTwoA, near * near, kTwoA), fmaf(-s, s, s), s);   // NaN where v is: s is
+                o.v[i] = from_f<T>(to_f(p[u][k].v[i]) * slope);
                 r.v[i] = from_f<T>(v * s);
             }
-            *reinterpret_cast<Pack<T, V> *>(dx + w.row * dxs + c) = o;
-            if (y) *reinterpret_cast<Pack<T, V> *>(y + w.row * ys + c) = r;
+            *reinterpret_cast<Pack<T, V> *>(dx + row[u] * dxs + c) = o;
+            if (y) *reinterpret_cast<Pack<T, V> *>(y + row[u] * ys + c) = r;
         }
     }
-}
-
-// As many blocks as the device holds at once, or as there is work for.
-inline int64_t grid_for(int64_t N, int64_t D, int lanes_per_group)
-{
-    const int64_t groups = N * ceil_div(D, kGroup), blocks = ceil_div(groups, kThreads / lanes_per_group);
-    const int64_t most = (int64_t)sm_count() * (2048 / kThreads);
-    return blocks < most ? blocks : most;
 }
 
 inline int check(int64_t N, int64_t D, int32_t dtype)
@@ -146,18 +225,40 @@ inline int check(int64_t N, int64_t D, int32_t dtype)
     return DC_OK;
 }
 
+// One row, where the rows follow each other without a gap and are whole groups: saves each thread the divisions, which cost as
+// much as 5 of its 32 elements (16384 x 8192 bf16: see the figures at the top).
+inline bool flatten(int64_t &N, int64_t &D, bool gapless)
+{
+    const bool flat = gapless && D % kGroup == 0;
+    if (flat) { D *= N; N = 1; }
+    return flat;
+}
+template <class T, int V> bool blocks_for(int64_t N, int64_t D, unsigned &blocks)
+{
+    const int64_t n = ceil_div(N * ceil_div(D, kGroup), Hold<T, V>::PER);
+    blocks = (unsigned)n;
+    return n <= INT32_MAX;
+}
+
 template <class T, int V>
 int forward(const void *x, int64_t xs, int64_t N, int64_t D, void *y, int64_t ys, int8_t *q, float *scales, cudaStream_t st)
 {
-    gelu_save8_kernel<T, V><<<(unsigned)grid_for(N, D, Hold<T, V>::LPG), kThreads, 0, st>>>((const T *)x, xs, N, (int32_t)D, (T *)y, ys, q, scales);
+    unsigned blocks;
+    const bool flat = flatten(N, D, V > 1 && xs == D && ys == D);
+    if (!blocks_for<T, V>(N, D, blocks)) return DC_ERR_RANGE;
+    if (flat) gelu_save8_kernel<T, V, V != 1><<<blocks, kThreads, 0, st>>>((const T *)x, xs, N, D, (T *)y, ys, q, scales);
+    else gelu_save8_kernel<T, V, false><<<blocks, kThreads, 0, st>>>((const T *)x, xs, N, D, (T *)y, ys, q, scales);
     return launched();
 }
 template <class T, int V>
 int backward(const void *dy, int64_t dys, const int8_t *q, const float *scales, int64_t N, int64_t D, void *dx, int64_t dxs, void *y, int64_t ys,
              cudaStream_t st)
 {
-    gelu_save8_backward_kernel<T, V><<<(unsigned)grid_for(N, D, Hold<T, V>::LPG), kThreads, 0, st>>>((const T *)dy, dys, q, scales, N, (int32_t)D,
-                                                                                                     (T *)dx, dxs, (T *)y, ys);
+    unsigned blocks;
+    const bool flat = flatten(N, D, V > 1 && dys == D && dxs == D && (!y || ys == D));
+    if (!blocks_for<T, V>(N, D, blocks)) return DC_ERR_RANGE;
+    if (flat) gelu_save8_backward_kernel<T, V, V != 1><<<blocks, kThreads, 0, st>>>((const T *)dy, dys, q, scales, N, D, (T *)dx, dxs, (T *)y, ys);
+    else gelu_save8_backward_kernel<T, V, false><<<blocks, kThreads, 0, st>>>((const T *)dy, dys, q, scales, N, D, (T *)dx, dxs, (T *)y, ys);
     return launched();
 }
 
@@ -174,7 +275,6 @@ extern "C" int dc_gelu_save8(const void *x, int64_t x_stride, int32_t dtype, int
     const int eb = elem_bytes(dtype), V = 16 / eb;
     if (x_stride < D || y_stride < D) return DC_ERR_SHAPE;
     if (!on(x, eb) || !on(y, eb) || !on(scales, 4)) return DC_ERR_ALIGN;
-    if (sm_count() == 0) return DC_ERR_CUDA;
     const bool wide = D % V == 0 && rows_on(x, x_stride, eb, 16) && rows_on(y, y_stride, eb, 16) && on(q, V);
     const cudaStream_t st = (cudaStream_t)stream;
     if (dtype == DC_BF16) return wide ? forward<__nv_bfloat16, 8>(x, x_stride, N, D, y, y_stride, q, scales, st)
@@ -193,7 +293,6 @@ extern "C" int dc_gelu_save8_backward(const void *dy, int64_t dy_stride, int32_t
     const int eb = elem_bytes(dtype), V = 16 / eb;
     if (dy_stride < D || dx_stride < D || (y_again && y_again_stride < D)) return DC_ERR_SHAPE;
     if (!on(dy, eb) || !on(dx, eb) || !on(y_again, eb) || !on(scales, 4)) return DC_ERR_ALIGN;
-    if (sm_count() == 0) return DC_ERR_CUDA;
     const bool wide = D % V == 0 && rows_on(dy, dy_stride, eb, 16) && rows_on(dx, dx_stride, eb, 16) &&
                       (!y_again || rows_on(y_again, y_again_stride, eb, 16)) && on(q, V);
     const cudaStream_t st = (cudaStream_t)stream;
