@@ -61,6 +61,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
                                                            uint8_t *__restrict__ occurs)
 {
     constexpr int U = 8;
+    follow();
     extern __shared__ int32_t hist[];                      // [keys]: how often each token of the bucket occurs, then where it goes
     __shared__ int32_t list_place[kList];
     __shared__ uint16_t list_key[kList];
@@ -226,6 +227,7 @@ __global__ void __launch_bounds__(128) embed_sum(const T *__restrict__ dout, int
 {
     constexpr int U = 8;                                   // rows on their way at a time
     const int lane = threadIdx.x & 31;
+    follow();
     if (blockIdx.x >= sum_blocks) {
         // rows of tokens that do not occur
         const int64_t step = (int64_t)(gridDim.x - sum_blocks) * 4;
@@ -293,6 +295,7 @@ __global__ void __launch_bounds__(128) embed_join(const int32_t *__restrict__ to
 {
     constexpr int U = 8;
     __shared__ float quarter[4][V][32];
+    follow();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t tile = blockIdx.x;
     const int32_t n = *live;
@@ -379,10 +382,9 @@ int backward_launch(const void *dout, int64_t ds, int64_t N, int64_t vocab, int6
     int64_t zeros = accumulate ? 0 : ceil_div(vocab, 4);
     if (zeros > (int64_t)sm_count() * 16) zeros = (int64_t)sm_count() * 16;
     if (sums + zeros > INT32_MAX || chunks > 65535) return DC_ERR_RANGE;
-    embed_sum<T, O, V><<<(unsigned)(sums + zeros), 128, 0, st>>>((const T *)dout, ds, w.place, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part,
-                                                                 w.pitch, chunks, sums, w.occurs, vocab);
-    embed_join<O, V><<<dim3((unsigned)tiles, (unsigned)chunks), 128, 0, st>>>(w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch);
-    return launched();
+    if (int e = launch(embed_sum<T, O, V>, dim3((unsigned)(sums + zeros)), 128, 0, st, (const T *)dout, ds, w.place, w.token, w.live, D, scale, (O *)dtable, ts,
+                       accumulate, w.part, w.pitch, chunks, sums, w.occurs, vocab)) return e;
+    return launch(embed_join<O, V>, dim3((unsigned)tiles, (unsigned)chunks), 128, 0, st, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch);
 }
 
 template <class T, int V>
@@ -453,7 +455,8 @@ extern "C" int dc_embed_backward(const void *dout, int64_t dout_stride, int32_t 
     const Work w = carve(workspace, N, V, D);
     const SortPlan p = sort_plan(V);
     if (pad_id < 0) pad_id = INT64_MIN;
-    embed_sort<<<1u << p.log_buckets, kSortThreads, (size_t)p.keys * 4, st>>>(ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token, w.live, accumulate ? nullptr : w.occurs);
+    if (int e = launch(embed_sort, dim3(1u << p.log_buckets), kSortThreads, (size_t)p.keys * 4, st, ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token,
+                       w.live, accumulate ? nullptr : w.occurs)) return e;
     // packs of V elements on both sides: 16 bytes of dout, and as many elements of dtable
     const int W = 16 / eb;
     const bool wide = D % W == 0 && rows_on(dout, dout_stride, eb, 16) && rows_on(dtable, dtable_stride, ob, (size_t)(W * ob));

@@ -3,15 +3,19 @@
 // Both kernels touch every element once (16-bit types: forward 2 bytes in, 2 + 1 out; backward 2 + 1 in, 2 + 2 out), so memory
 // bounds them as long as an element costs less than about 25 instructions, 3 of them on the special-function unit.  A group of
 // 128 is held by 128/V lanes with V adjacent elements each (V = 16 bytes' worth), which makes its maximum a few shuffles and
-// leaves nothing to pass through shared memory; a thread has kAhead groups on their way at once.  Conversions between integers
-// and floats, which would go to the special-function unit too, are done by adding a constant whose last bits are the integer.
+// leaves nothing to pass through shared memory.  Conversions between integers and floats, which would go to the
+// special-function unit too, are done by adding a constant whose last bits are the integer.
 #include "train_common.cuh"
 
 namespace dct {
 
 constexpr int kGroup = DC_SAVE8_GROUP;
-constexpr int kThreads = 256;
-constexpr int kAhead = 4;
+// Blocks of 128 threads; a thread has two groups on their way in the forward pass and one in the backward pass.  16384 x 8192
+// bf16, us forward / backward: 128 threads 124 / 152 (one group), 117 / 162 (two), 118 / 162 (four); 256 threads 126 / 152, 120 /
+// 166, 127 / 175; 512 threads 128 / 156 (one).  Memory takes 3.7 TB/s when it is only written (fill of 268 MB: 72 us), so the
+// bytes written alone need 109 / 145.
+constexpr int kThreads = 128;
+constexpr int kAheadForward = 2, kAheadBackward = 1;
 constexpr float kTwoA = 1.5957691216057308f;                   // 2 sqrt(2/pi)
 constexpr float kB = 0.044715f;
 constexpr float kLog2E = 1.4426950408889634f;
@@ -79,7 +83,7 @@ template <> struct Top<float> {
 
 // How the lanes of a warp hold a group: packs of V elements, LPG lanes to a group, K packs to a lane.  A block has PER groups on
 // their way, a thread every GAP-th of them.
-template <class T, int V> struct Hold {
+template <class T, int V, int kAhead> struct Hold {
     static constexpr int LPG = kGroup / V < 32 ? kGroup / V : 32;
     static constexpr int K = kGroup / (V * LPG);
     static constexpr int GAP = kThreads / LPG, PER = GAP * kAhead;
@@ -115,7 +119,8 @@ template <class T, int V, bool FLAT>
 __global__ void __launch_bounds__(kThreads) gelu_save8_kernel(const T *__restrict__ x, int64_t xs, int64_t N, int64_t D, T *__restrict__ y, int64_t ys,
                                                               int8_t *__restrict__ q, float *__restrict__ scales)
 {
-    using H = Hold<T, V>;
+    constexpr int kAhead = kAheadForward;
+    using H = Hold<T, V, kAhead>;
     const int lane = threadIdx.x % H::LPG;
     const int64_t per_row = (D + kGroup - 1) / kGroup, first = (int64_t)blockIdx.x * H::PER + threadIdx.x / H::LPG;
     Groups<FLAT> g(first, H::GAP, per_row, D);
@@ -173,7 +178,8 @@ __global__ void __launch_bounds__(kThreads) gelu_save8_backward_kernel(const T *
                                                                        const float *__restrict__ scales, int64_t N, int64_t D, T *__restrict__ dx,
                                                                        int64_t dxs, T *__restrict__ y, int64_t ys)
 {
-    using H = Hold<T, V>;
+    constexpr int kAhead = kAheadBackward;
+    using H = Hold<T, V, kAhead>;
     const int lane = threadIdx.x % H::LPG;
     const int64_t per_row = (D + kGroup - 1) / kGroup, first = (int64_t)blockIdx.x * H::PER + threadIdx.x / H::LPG;
     Groups<FLAT> g(first, H::GAP, per_row, D);
@@ -233,9 +239,9 @@ inline bool flatten(int64_t &N, int64_t &D, bool gapless)
     if (flat) { D *= N; N = 1; }
     return flat;
 }
-template <class T, int V> bool blocks_for(int64_t N, int64_t D, unsigned &blocks)
+template <class H> bool blocks_for(int64_t N, int64_t D, unsigned &blocks)
 {
-    const int64_t n = ceil_div(N * ceil_div(D, kGroup), Hold<T, V>::PER);
+    const int64_t n = ceil_div(N * ceil_div(D, kGroup), H::PER);
     blocks = (unsigned)n;
     return n <= INT32_MAX;
 }
@@ -245,7 +251,7 @@ int forward(const void *x, int64_t xs, int64_t N, int64_t D, void *y, int64_t ys
 {
     unsigned blocks;
     const bool flat = flatten(N, D, V > 1 && xs == D && ys == D);
-    if (!blocks_for<T, V>(N, D, blocks)) return DC_ERR_RANGE;
+    if (!blocks_for<Hold<T, V, kAheadForward>>(N, D, blocks)) return DC_ERR_RANGE;
     if (flat) gelu_save8_kernel<T, V, V != 1><<<blocks, kThreads, 0, st>>>((const T *)x, xs, N, D, (T *)y, ys, q, scales);
     else gelu_save8_kernel<T, V, false><<<blocks, kThreads, 0, st>>>((const T *)x, xs, N, D, (T *)y, ys, q, scales);
     return launched();
@@ -256,7 +262,7 @@ int backward(const void *dy, int64_t dys, const int8_t *q, const float *scales, 
 {
     unsigned blocks;
     const bool flat = flatten(N, D, V > 1 && dys == D && dxs == D && (!y || ys == D));
-    if (!blocks_for<T, V>(N, D, blocks)) return DC_ERR_RANGE;
+    if (!blocks_for<Hold<T, V, kAheadBackward>>(N, D, blocks)) return DC_ERR_RANGE;
     if (flat) gelu_save8_backward_kernel<T, V, V != 1><<<blocks, kThreads, 0, st>>>((const T *)dy, dys, q, scales, N, D, (T *)dx, dxs, (T *)y, ys);
     else gelu_save8_backward_kernel<T, V, false><<<blocks, kThreads, 0, st>>>((const T *)dy, dys, q, scales, N, D, (T *)dx, dxs, (T *)y, ys);
     return launched();

@@ -36,6 +36,29 @@ inline bool on(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p)
 // rows of a matrix whose starts all fall on `a`-byte boundaries
 inline bool rows_on(const void *p, int64_t stride, int eb, size_t a) { return on(p, a) && (size_t)(stride * eb) % a == 0; }
 
+// Kernels of one call follow each other with programmatic dependent launch: the next one may start, and set itself up, while
+// the last blocks of the one before still run, and waits in follow() until that one is done and its writes are visible.  Every
+// kernel calls it before it touches global memory, so all that went before in the stream is done too.
+template <class... P, class... A> int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args)
+{
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid;
+    c.blockDim = dim3((unsigned)threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...) == cudaSuccess ? DC_OK : DC_ERR_CUDA;
+}
+__device__ __forceinline__ void follow()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // A pack of adjacent elements of a row: 16 bytes where rows start on 16-byte boundaries, one element otherwise.
 template <class T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
 

@@ -20,12 +20,15 @@ namespace dct {
 constexpr int kTileM = 256, kTileN = 256;   // rows and columns of a tile of the result
 constexpr int kRowBlock = 64;               // elements of the summed dimension to a stage of the ring
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // g of one piece of the vocabulary
-constexpr int kStages = 6, kStageBytes = 2 * 128 * 64 * 2;
+constexpr int kStageBytes = 2 * 128 * 64 * 2;
 constexpr int kTcThreads = 384;             // warp 0 copies, warp 1 multiplies, warp 2 has the tensor memory, warps 4-11 take tiles out
-constexpr int kTcSmem = kStages * kStageBytes + 1024;
 constexpr int kMaxParts = 16;
 
 enum What { kLoss, kGrad, kBack };
+// kBack passes its tiles through shared memory, 32 x 32 to a warp, so that it has room for a stage less
+constexpr int kPitch = 36;                  // floats to a row there: 16-byte accesses of a row each and along rows meet no bank twice
+__host__ __device__ constexpr int stages_of(int what) { return what == kBack ? 5 : 6; }
+__host__ __device__ constexpr int smem_of(int what) { return 1024 + stages_of(what) * kStageBytes + (what == kBack ? 8 * 32 * kPitch * 4 : 0); }
 
 // What vocab_gather finds out on the device.
 struct Head {
@@ -171,43 +174,40 @@ __device__ __forceinline__ void online(const float (&v)[32], int32_t valid, floa
     s = a + b;
 }
 
-template <class T>
-__device__ __forceinline__ void put_weight_grad(const Product &p, int32_t row, int32_t col, const float (&v)[32], float unscale)
+// 32 x 32 results of a warp, a row to a thread, to rows of `to` that are `stride` apart: times `f`, added or not.  They change
+// places in shared memory, so that neighbouring threads write neighbouring elements: written from the rows' own threads, 8 tokens
+// x 32000 x 1024 took 50 us.
+// wide: rows start on 16-byte boundaries.
+template <class O>
+__device__ __forceinline__ void put_tile(float *room, const float (&v)[32], O *to, int64_t stride, int32_t rows, int32_t cols, float f, bool add, bool wide)
 {
-    if (row >= p.V || col >= p.D) return;
-    const int64_t at = (int64_t)row * p.dw_stride + col;
-    if (p.dw_wide && col + 32 <= p.D) {
-        if (p.dw_f32) {
-            float4 *o = reinterpret_cast<float4 *>((float *)p.dw + at);
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float4 x = make_float4(v[4 * i] * unscale, v[4 * i + 1] * unscale, v[4 * i + 2] * unscale, v[4 * i + 3] * unscale);
-                if (p.dw_add) { const float4 y = o[i]; x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w; }
-                o[i] = x;
-            }
-        } else {
-            Pack<T, 8> *o = reinterpret_cast<Pack<T, 8> *>((T *)p.dw + at);
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<float4 *>(room + lane * kPitch + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    __syncwarp();
+    if (wide && cols >= 32) {
+        const int r0 = lane >> 3, c = (lane & 7) * 4;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                Pack<T, 8> x;
-                if (p.dw_add) x = o[i];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x.v[j] = from_f<T>((p.dw_add ? to_f(x.v[j]) : 0.0f) + v[8 * i + j] * unscale);
-                o[i] = x;
-            }
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + r0;
+            if (r >= rows) continue;
+            const float4 x = *reinterpret_cast<const float4 *>(room + r * kPitch + c);
+            Pack<O, 4> *o = reinterpret_cast<Pack<O, 4> *>(to + r * stride + c), y;
+            if (add) y = *o;
+            y.v[0] = from_f<O>((add ? to_f(y.v[0]) : 0.0f) + x.x * f);
+            y.v[1] = from_f<O>((add ? to_f(y.v[1]) : 0.0f) + x.y * f);
+            y.v[2] = from_f<O>((add ? to_f(y.v[2]) : 0.0f) + x.z * f);
+            y.v[3] = from_f<O>((add ? to_f(y.v[3]) : 0.0f) + x.w * f);
+            *o = y;
         }
         return;
     }
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        if (col + i >= p.D) break;
-        if (p.dw_f32) {
-            float *o = (float *)p.dw + at + i;
-            *o = (p.dw_add ? *o : 0.0f) + v[i] * unscale;
-        } else {
-            T *o = (T *)p.dw + at + i;
-            *o = from_f<T>((p.dw_add ? to_f(*o) : 0.0f) + v[i] * unscale);
-        }
+    if (lane >= cols) return;
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r) {
+        O *o = to + r * stride + lane;
+        *o = from_f<O>((add ? to_f(*o) : 0.0f) + room[r * kPitch + lane] * f);
     }
 }
 
@@ -219,7 +219,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
 vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUtensorMap b, const __grid_constant__ CUtensorMap a_dw,
               const __grid_constant__ CUtensorMap b_dw, const __grid_constant__ Product p)
 {
-    constexpr bool kBf16 = sizeof(T) == 2 && !__is_same(T, __half);
+    constexpr bool kBf16 = !__is_same(T, __half);
+    constexpr int kStages = stages_of(WHAT);
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t full[kStages], empty[kStages], ready[2], taken[2];
     __shared__ uint32_t tmem_at;
@@ -246,6 +247,7 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
     cluster_sync();
     tc_after_sync();
     const uint32_t tmem = tmem_at;
+    follow();
     const Units<WHAT> units(p);
 
     if (warp == 0 && lane == 0) {
@@ -371,23 +373,19 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
                         for (int i = 0; i < 8; ++i) r[i] = pack2(v[h * 16 + 2 * i], v[h * 16 + 2 * i + 1], T());
                         store32(o + h * 16, r);
                     }
-                } else if (t.dw) {
-                    put_weight_grad<T>(p, row, col, v, unscale);
-                } else if (row < units.rows && col < p.Dp && (t.blocks > 0 || p.first)) {
-                    float *o = p.acc + ((int64_t)t.part * units.rows + row) * p.Dp + col;
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        if (!p.first) {
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const float4 y = reinterpret_cast<const float4 *>(o + h * 8)[i];
-                                v[h * 8 + i * 4] += y.x; v[h * 8 + i * 4 + 1] += y.y; v[h * 8 + i * 4 + 2] += y.z; v[h * 8 + i * 4 + 3] += y.w;
-                            }
-                        }
-                        uint32_t r[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[h * 8 + i]);
-                        store32(o + h * 8, r);
+                } else {
+                    float *room = reinterpret_cast<float *>(raw + (ring - smem_u32(raw)) + kStages * kStageBytes) + (warp - 4) * 32 * kPitch;
+                    const int32_t row0 = row - lane;
+                    if (t.dw) {
+                        const int32_t r = min(32, p.V - row0), c = p.D - col;
+                        const int64_t at = (int64_t)row0 * p.dw_stride + col;
+                        if (r <= 0 || c <= 0) continue;
+                        if (p.dw_f32) put_tile(room, v, (float *)p.dw + at, p.dw_stride, r, c, unscale, p.dw_add, p.dw_wide);
+                        else put_tile(room, v, (T *)p.dw + at, p.dw_stride, r, c, unscale, p.dw_add, p.dw_wide);
+                    } else {
+                        const int32_t r = min(32, units.rows - row0);
+                        if (r <= 0 || col >= p.Dp || (t.blocks == 0 && !p.first)) continue;
+                        put_tile(room, v, p.acc + ((int64_t)t.part * units.rows + row0) * p.Dp + col, p.Dp, r, 32, 1.0f, !p.first, true);
                     }
                 }
             }
@@ -423,12 +421,13 @@ template <class T> int32_t pairs_on_device()
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     const int32_t have = __atomic_load_n(&cached[dev], __ATOMIC_ACQUIRE);
     if (have) return have;
-    for (auto f : {vocab_product<T, kLoss>, vocab_product<T, kGrad>, vocab_product<T, kBack>})
-        if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem) != cudaSuccess) return 0;
+    if (cudaFuncSetAttribute(vocab_product<T, kLoss>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kLoss)) != cudaSuccess ||
+        cudaFuncSetAttribute(vocab_product<T, kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kGrad)) != cudaSuccess ||
+        cudaFuncSetAttribute(vocab_product<T, kBack>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kBack)) != cudaSuccess) return 0;
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3((unsigned)sm_count() & ~1u);
     c.blockDim = dim3(kTcThreads);
-    c.dynamicSmemBytes = kTcSmem;
+    c.dynamicSmemBytes = smem_of(kBack);
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = 2;
@@ -436,7 +435,7 @@ template <class T> int32_t pairs_on_device()
     c.attrs = at;
     c.numAttrs = 1;
     int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, vocab_product<T, kLoss>, &c) != cudaSuccess || n <= 0) return 0;
+    if (cudaOccupancyMaxActiveClusters(&n, vocab_product<T, kBack>, &c) != cudaSuccess || n <= 0) return 0;
     __atomic_store_n(&cached[dev], n, __ATOMIC_RELEASE);
     return n;
 }
@@ -451,8 +450,7 @@ int launch_units(int64_t most_units, int32_t pairs, const CUtensorMap &a, const 
                  cudaStream_t st)
 {
     const int64_t n = most_units < pairs ? most_units : pairs;
-    vocab_product<T, WHAT><<<(unsigned)(2 * (n > 0 ? n : 1)), kTcThreads, kTcSmem, st>>>(a, b, a_dw, b_dw, p);
-    return launched();
+    return launch(vocab_product<T, WHAT>, dim3((unsigned)(2 * (n > 0 ? n : 1))), kTcThreads, smem_of(WHAT), st, a, b, a_dw, b_dw, p);
 }
 
 }  // namespace dct

@@ -15,7 +15,7 @@
 
 namespace dct {
 
-constexpr int kGatherBlocks = 256;
+constexpr int kGatherBlocks = 256, kGatherThreads = 512;
 
 // ---- taking out the labelled rows ------------------------------------------------------------------------------------------
 
@@ -35,24 +35,34 @@ struct Gather {
 // Every block counts the labelled rows before its own, and in the backward pass finds the largest factor |dloss c|, by itself:
 // a few bytes per row from L2, and no block waits for another.
 template <class T, int V>
-__global__ void __launch_bounds__(256) vocab_gather(Gather a)
+__global__ void __launch_bounds__(kGatherThreads) vocab_gather(const __grid_constant__ Gather a)
 {
-    __shared__ int32_t count[8];
-    __shared__ float top[8];
+    constexpr int W = kGatherThreads / 32, U = 4;
+    __shared__ int32_t count[W];
+    __shared__ float top[W];
     __shared__ int32_t where[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t first = (int64_t)blockIdx.x * a.per_block, end = min(a.N, first + a.per_block);
     const bool last_block = blockIdx.x == gridDim.x - 1;
+    follow();
     int32_t c = 0;
     float m = 0.0f;
     const int64_t look = a.dloss ? a.N : first;
-#pragma unroll 4
-    for (int64_t i = tid; i < look; i += 256) {
-        const int64_t t = a.targets[i];
-        const bool ok = t != a.ignore && t >= 0 && t < a.V;
-        const float d = a.dloss ? a.dloss[i] : 0.0f;
-        c += ok && i < first;
-        m = ok ? fmaxf(m, fabsf(d * a.logit_scale)) : m;
+    for (int64_t i0 = tid; i0 < look; i0 += 8 * kGatherThreads) {
+        int64_t t[8];
+        float d[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int64_t i = i0 + u * kGatherThreads;
+            t[u] = i < look ? a.targets[i] : a.ignore;
+            d[u] = a.dloss && i < look ? a.dloss[i] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const bool ok = t[u] != a.ignore && t[u] >= 0 && t[u] < a.V;
+            c += ok && i0 + u * kGatherThreads < first;
+            m = ok ? fmaxf(m, fabsf(d[u] * a.logit_scale)) : m;
+        }
     }
     c = __reduce_add_sync(~0u, c);
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
@@ -60,7 +70,7 @@ __global__ void __launch_bounds__(256) vocab_gather(Gather a)
     __syncthreads();
     int32_t base = 0;
     m = 0.0f;
-    for (int w = 0; w < 8; ++w) { base += count[w]; m = fmaxf(m, top[w]); }
+    for (int w = 0; w < W; ++w) { base += count[w]; m = fmaxf(m, top[w]); }
     if (!(m > 0.0f && m < INFINITY)) m = 1.0f;
     const T *hidden = (const T *)a.hidden;
     T *rows = (T *)a.rows;
@@ -88,14 +98,23 @@ __global__ void __launch_bounds__(256) vocab_gather(Gather a)
         }
         base += __popc(all);
         __syncthreads();
-        for (int j = warp; j < 32; j += 8) {
+        for (int j = warp; j < 32; j += W) {
             const int32_t to = where[j];
             if (to < 0) continue;
             const T *from = hidden + (i0 + j) * a.hs;
-            for (int32_t d = lane * V; d < a.Dp; d += 32 * V) {
-                Pack<T, V> x = {};
-                if (d < a.D) x = *reinterpret_cast<const Pack<T, V> *>(from + d);
-                *reinterpret_cast<Pack<T, V> *>(rows + (int64_t)to * a.Dp + d) = x;
+            for (int32_t d0 = lane * V; d0 < a.Dp; d0 += 32 * V * U) {
+                Pack<T, V> x[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int32_t d = d0 + u * 32 * V;
+                    x[u] = Pack<T, V>{};
+                    if (d < a.D) x[u] = *reinterpret_cast<const Pack<T, V> *>(from + d);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int32_t d = d0 + u * 32 * V;
+                    if (d < a.Dp) *reinterpret_cast<Pack<T, V> *>(rows + (int64_t)to * a.Dp + d) = x[u];
+                }
             }
         }
         __syncthreads();
@@ -109,7 +128,7 @@ __global__ void __launch_bounds__(256) vocab_gather(Gather a)
     // dW is summed over whole blocks of kRowBlock rows: what follows the last row there is zero
     if (a.dloss) {
         const int64_t from = (int64_t)base * a.Dp, to = ceil_div(base, kRowBlock) * kRowBlock * (int64_t)a.Dp;
-        for (int64_t d = from + tid * 8; d < to; d += 256 * 8) *reinterpret_cast<uint4 *>(rows + d) = make_uint4(0, 0, 0, 0);
+        for (int64_t d = from + tid * 8; d < to; d += kGatherThreads * 8) *reinterpret_cast<uint4 *>(rows + d) = make_uint4(0, 0, 0, 0);
     }
 }
 
@@ -117,6 +136,7 @@ __global__ void __launch_bounds__(256) vocab_gather(Gather a)
 template <class T>
 __global__ void __launch_bounds__(256) vocab_copy_weight(const T *__restrict__ w, int64_t ws, int64_t V, int32_t D, int32_t Dp, T *__restrict__ to)
 {
+    follow();
     for (int64_t v = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); v < V; v += (int64_t)gridDim.x * 8)
         for (int32_t d = threadIdx.x & 31; d < Dp; d += 32) to[v * Dp + d] = d < D ? w[v * ws + d] : from_f<T>(0.0f);
 }
@@ -128,6 +148,7 @@ __global__ void __launch_bounds__(256) vocab_join(const Head *__restrict__ head,
 {
     const int lane = threadIdx.x & 31;
     const int64_t j = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    follow();
     if (j >= head->rows) return;
     const float2 *p = part + j * tiles;
     float m = -INFINITY, s = 0.0f;                          // in powers of two, as the tiles are
@@ -151,33 +172,40 @@ __global__ void __launch_bounds__(256) vocab_join(const Head *__restrict__ head,
 
 // ---- the gradient of the hidden states: partial products joined in order and put back to their rows ------------------------
 
+// A warp takes (row, 32 V columns), four of the partial products on their way at a time.
 template <class T, int V>
 __global__ void __launch_bounds__(256) vocab_put_back(const Head *__restrict__ head, const int32_t *__restrict__ pos_of, const int32_t *__restrict__ label,
                                                       const float *__restrict__ rest, const float *__restrict__ acc, const T *__restrict__ w, int64_t ws, int64_t N,
-                                                      int32_t D, int32_t Dp, float unscale, T *__restrict__ out, int64_t os)
+                                                      int32_t D, int32_t Dp, float unscale, T *__restrict__ out, int64_t os, int32_t chunks)
 {
-    const int64_t n = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (n >= N) return;
-    const int32_t p = pos_of[n], rows = head->rows, parts = head->parts;
-    const float f = head->top * unscale, r = p >= 0 ? rest[p] : 0.0f;
-    const T *at_label = p >= 0 ? w + label[p] * ws : w;
-    for (int32_t d = (threadIdx.x & 31) * V; d < D; d += 32 * V) {
-        Pack<T, V> o = {};
-        if (p >= 0) {
-            float s[V];
-            const Pack<T, V> l = *reinterpret_cast<const Pack<T, V> *>(at_label + d);
+    constexpr int U = 4;
+    follow();
+    const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n = task / chunks;
+    const int32_t d = (int32_t)(task - n * chunks) * (32 * V) + (threadIdx.x & 31) * V;
+    if (n >= N || d >= D) return;
+    const int32_t p = pos_of[n];
+    Pack<T, V> o = {};
+    if (p >= 0) {
+        const int32_t rows = head->rows, parts = head->parts;
+        const float f = head->top * unscale, r = rest[p];
+        const Pack<T, V> l = *reinterpret_cast<const Pack<T, V> *>(w + label[p] * ws + d);
+        float s[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[i] = r * to_f(l.v[i]);
-            for (int32_t k = 0; k < parts; ++k) {
-                const Pack<float, V> x = *reinterpret_cast<const Pack<float, V> *>(acc + ((int64_t)k * rows + p) * Dp + d);
+        for (int i = 0; i < V; ++i) s[i] = r * to_f(l.v[i]);
+        for (int32_t k = 0; k < parts; k += U) {
+            Pack<float, V> x[U];
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[i] += x.v[i];
-            }
+            for (int u = 0; u < U; ++u)
+                if (k + u < parts) x[u] = *reinterpret_cast<const Pack<float, V> *>(acc + ((int64_t)(k + u) * rows + p) * Dp + d);
 #pragma unroll
-            for (int i = 0; i < V; ++i) o.v[i] = from_f<T>(s[i] * f);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[i] += k + u < parts ? x[u].v[i] : 0.0f;
         }
-        *reinterpret_cast<Pack<T, V> *>(out + n * os + d) = o;
+#pragma unroll
+        for (int i = 0; i < V; ++i) o.v[i] = from_f<T>(s[i] * f);
     }
+    *reinterpret_cast<Pack<T, V> *>(out + n * os + d) = o;
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------------
@@ -244,19 +272,19 @@ int gather(Gather &g, cudaStream_t st)
 {
     g.per_block = (int32_t)(ceil_div(ceil_div(g.N, kGatherBlocks), 32) * 32);
     const unsigned blocks = (unsigned)ceil_div(g.N, g.per_block);
-    if (g.D % 8 == 0 && rows_on(g.hidden, g.hs, 2, 16)) vocab_gather<T, 8><<<blocks, 256, 0, st>>>(g);
-    else vocab_gather<T, 1><<<blocks, 256, 0, st>>>(g);
-    return launched();
+    const bool wide = g.D % 8 == 0 && rows_on(g.hidden, g.hs, 2, 16);
+    return launch(wide ? vocab_gather<T, 8> : vocab_gather<T, 1>, dim3(blocks), kGatherThreads, 0, st, g);
 }
 
 // The weight as bulk tensor copies can read it.
 template <class T>
-void readable(const Plan &p, const Gather &g, const void **weight, int64_t *ws, cudaStream_t st)
+int readable(const Plan &p, const Gather &g, const void **weight, int64_t *ws, cudaStream_t st)
 {
-    if (!p.copy_weight) return;
-    vocab_copy_weight<T><<<(unsigned)(sm_count() * 8), 256, 0, st>>>((const T *)*weight, *ws, g.V, g.D, p.Dp, (T *)p.weight);
+    if (!p.copy_weight) return DC_OK;
+    const int e = launch(vocab_copy_weight<T>, dim3((unsigned)(sm_count() * 8)), 256, 0, st, (const T *)*weight, *ws, g.V, g.D, p.Dp, (T *)p.weight);
     *weight = p.weight;
     *ws = p.Dp;
+    return e;
 }
 
 template <class T>
@@ -270,12 +298,11 @@ int forward(Gather g, const Plan &p, const void *weight, int64_t ws, float *loss
     if (!tensor_map(&a, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&b, p.copy_weight ? p.weight : weight, bf, g.D, g.V, p.copy_weight ? p.Dp : ws, 128))
         return DC_ERR_CUDA;
     if (int e = gather<T>(g, st)) return e;
-    readable<T>(p, g, &weight, &ws, st);
+    if (int e = readable<T>(p, g, &weight, &ws, st)) return e;
     q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.part = p.part; q.hit = p.hit; q.part_pitch = 2 * p.tiles_v;
     q.V = (int32_t)g.V; q.D = g.D; q.Dp = p.Dp;
     if (int e = launch_units<T, kLoss>(p.Lp / kTileM * p.tiles_v, pairs, a, b, a, b, q, st)) return e;
-    vocab_join<<<(unsigned)ceil_div(g.N, 8), 256, 0, st>>>(p.head, p.row_of, p.part, p.hit, 2 * p.tiles_v, loss, lse);
-    return launched();
+    return launch(vocab_join, dim3((unsigned)ceil_div(g.N, 8)), 256, 0, st, p.head, p.row_of, p.part, p.hit, 2 * p.tiles_v, loss, lse);
 }
 
 template <class T>
@@ -286,7 +313,7 @@ int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, 
     if (pairs == 0) return DC_ERR_CUDA;
     g.vocab_blocks = p.vocab_blocks; g.pairs = pairs; g.acc_rows = p.acc_rows;
     if (int e = gather<T>(g, st)) return e;
-    readable<T>(p, g, &weight, &ws, st);
+    if (int e = readable<T>(p, g, &weight, &ws, st)) return e;
     const int ob = dw_f32 ? 4 : 2;
     CUtensorMap rows, rows_mn, grad_k, grad_mn;
     if (!tensor_map(&rows, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&grad_k, p.grad, bf, p.piece, p.Lp, p.piece, 128) ||
@@ -312,11 +339,12 @@ int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, 
         if (int e = launch_units<T, kBack>(units, pairs, grad_k, w_mn, grad_mn, rows_mn, q, st)) return e;
     }
     if (!dh) return DC_OK;
-    const unsigned blocks = (unsigned)ceil_div(g.N, 8);
-    const float unscale = 1.0f / grad_scale<T>();
-    if (g.D % 4 == 0 && rows_on(dh, dhs, 2, 8) && rows_on(weight, ws, 2, 8)) vocab_put_back<T, 4><<<blocks, 256, 0, st>>>(p.head, p.pos_of, p.label, p.rest, p.acc, (const T *)weight, ws, g.N, g.D, p.Dp, unscale, (T *)dh, dhs);
-    else vocab_put_back<T, 1><<<blocks, 256, 0, st>>>(p.head, p.pos_of, p.label, p.rest, p.acc, (const T *)weight, ws, g.N, g.D, p.Dp, unscale, (T *)dh, dhs);
-    return launched();
+    const bool wide = g.D % 8 == 0 && rows_on(dh, dhs, 2, 16) && rows_on(weight, ws, 2, 16);
+    const int32_t chunks = (int32_t)ceil_div(g.D, wide ? 256 : 32);
+    const int64_t blocks = ceil_div(g.N * chunks, 8);
+    if (blocks > INT32_MAX) return DC_ERR_RANGE;
+    return launch(wide ? vocab_put_back<T, 8> : vocab_put_back<T, 1>, dim3((unsigned)blocks), 256, 0, st, p.head, p.pos_of, p.label, p.rest, p.acc,
+                  (const T *)weight, ws, g.N, g.D, p.Dp, 1.0f / grad_scale<T>(), (T *)dh, dhs, chunks);
 }
 
 }  // namespace dct
