@@ -42,21 +42,23 @@ struct Head {
 // the shortest longest list are taken.  Each unit is charged kUnitCost blocks for taking its tile out.  The tiles of dW count
 // whether dW is asked for or not, so that dh has the same bits either way.
 constexpr uint32_t kUnitCost = 6;
-__host__ __device__ inline uint32_t up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
-__host__ __device__ inline int32_t parts_of(uint32_t rows, uint32_t D, uint32_t vocab_blocks, uint32_t pairs, int64_t acc_rows)
+__device__ inline uint32_t up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
+// called by a whole warp: a lane weighs one number of parts
+__device__ inline int32_t parts_of(uint32_t rows, uint32_t D, uint32_t vocab_blocks, uint32_t pairs, int64_t acc_rows)
 {
-    if (rows == 0) return 1;
-    const uint32_t td = up(D, kTileN), rb = up(rows, kRowBlock) + kUnitCost;
+    const uint32_t s = (threadIdx.x & 31) + 1, td = up(D, kTileN), rb = up(rows, kRowBlock) + kUnitCost;
     const uint32_t nw = up(vocab_blocks, kTileM / kRowBlock) * td, q = nw / pairs, r = nw % pairs;
-    uint32_t best = 1;
-    uint64_t least = ~0ull;
-    for (uint32_t s = 1; s <= kMaxParts && s <= vocab_blocks && (int64_t)s * rows <= acc_rows; ++s) {
-        const uint32_t len = up(vocab_blocks, s);
-        if (up(vocab_blocks, len) != s) continue;                       // the last part would be empty
-        const uint32_t cost = len + kUnitCost, n = up(rows, kTileM) * td * s, q2 = n / pairs, r2 = n % pairs, dw = r ? rb : 0, dh = r2 ? cost : 0;
-        const uint32_t extra = r + r2 > pairs ? dw + dh : dw > dh ? dw : dh;
-        const uint64_t total = (uint64_t)q * rb + (uint64_t)q2 * cost + extra;
-        if (total < least) { least = total; best = s; }
+    const uint32_t len = up(vocab_blocks, s), cost = len + kUnitCost, n = up(rows, kTileM) * td * s, q2 = n / pairs, r2 = n % pairs;
+    const uint32_t dw = r ? rb : 0, dh = r2 ? cost : 0, extra = r + r2 > pairs ? dw + dh : max(dw, dh);
+    uint64_t total = (uint64_t)q * rb + (uint64_t)q2 * cost + extra;
+    // s parts of `len` blocks have to leave none empty, and their sums have to fit
+    if (s > 1 && (s > kMaxParts || s > vocab_blocks || (int64_t)s * rows > acc_rows || up(vocab_blocks, len) != s)) total = ~0ull;
+    uint32_t best = s;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        const uint64_t o = __shfl_xor_sync(~0u, total, d);
+        const uint32_t b = __shfl_xor_sync(~0u, best, d);
+        if (o < total || (o == total && b < best)) { total = o; best = b; }
     }
     return (int32_t)best;
 }
@@ -175,40 +177,48 @@ __device__ __forceinline__ void online(const float (&v)[32], int32_t valid, floa
 }
 
 // 32 x 32 results of a warp, a row to a thread, to rows of `to` that are `stride` apart: times `f`, added or not.  They change
-// places in shared memory, so that neighbouring threads write neighbouring elements: written from the rows' own threads, 8 tokens
-// x 32000 x 1024 took 50 us.
-// wide: rows start on 16-byte boundaries.
-template <class O>
-__device__ __forceinline__ void put_tile(float *room, const float (&v)[32], O *to, int64_t stride, int32_t rows, int32_t cols, float f, bool add, bool wide)
+// places in shared memory, so that neighbouring threads write neighbouring elements.  wide: rows start on 16-byte boundaries.
+template <class O, bool ADD>
+__device__ __forceinline__ void put_tile(float *room, const float (&v)[32], O *to, int64_t stride, int32_t rows, int32_t cols, float f, bool wide)
 {
     const int lane = threadIdx.x & 31;
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 8; ++i) *reinterpret_cast<float4 *>(room + lane * kPitch + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
     __syncwarp();
-    if (wide && cols >= 32) {
-        const int r0 = lane >> 3, c = (lane & 7) * 4;
+    if (wide && rows >= 32 && cols >= 32) {
+        // four rows of 32 at a time: eight threads to a row
+        const float *from = room + (lane >> 3) * kPitch + (lane & 7) * 4;
+        O *o = to + (lane >> 3) * stride + (lane & 7) * 4;
+        float4 x[8];
+        Pack<O, 4> y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int r = i * 4 + r0;
-            if (r >= rows) continue;
-            const float4 x = *reinterpret_cast<const float4 *>(room + r * kPitch + c);
-            Pack<O, 4> *o = reinterpret_cast<Pack<O, 4> *>(to + r * stride + c), y;
-            if (add) y = *o;
-            y.v[0] = from_f<O>((add ? to_f(y.v[0]) : 0.0f) + x.x * f);
-            y.v[1] = from_f<O>((add ? to_f(y.v[1]) : 0.0f) + x.y * f);
-            y.v[2] = from_f<O>((add ? to_f(y.v[2]) : 0.0f) + x.z * f);
-            y.v[3] = from_f<O>((add ? to_f(y.v[3]) : 0.0f) + x.w * f);
-            *o = y;
+            x[i] = *reinterpret_cast<const float4 *>(from + i * 4 * kPitch);
+            if (ADD) y[i] = *reinterpret_cast<const Pack<O, 4> *>(o + i * (4 * stride));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            y[i].v[0] = from_f<O>(ADD ? fmaf(x[i].x, f, to_f(y[i].v[0])) : x[i].x * f);
+            y[i].v[1] = from_f<O>(ADD ? fmaf(x[i].y, f, to_f(y[i].v[1])) : x[i].y * f);
+            y[i].v[2] = from_f<O>(ADD ? fmaf(x[i].z, f, to_f(y[i].v[2])) : x[i].z * f);
+            y[i].v[3] = from_f<O>(ADD ? fmaf(x[i].w, f, to_f(y[i].v[3])) : x[i].w * f);
+            *reinterpret_cast<Pack<O, 4> *>(o + i * (4 * stride)) = y[i];
         }
         return;
     }
     if (lane >= cols) return;
-#pragma unroll 8
-    for (int r = 0; r < rows; ++r) {
-        O *o = to + r * stride + lane;
-        *o = from_f<O>((add ? to_f(*o) : 0.0f) + room[r * kPitch + lane] * f);
+    O *o = to + lane;
+    for (int r = 0; r < rows; ++r, o += stride) {
+        const float x = room[r * kPitch + lane];
+        *o = from_f<O>(ADD ? fmaf(x, f, to_f(*o)) : x * f);
     }
+}
+template <class O>
+__device__ __forceinline__ void put_tile(float *room, const float (&v)[32], O *to, int64_t stride, int32_t rows, int32_t cols, float f, bool add, bool wide)
+{
+    if (add) put_tile<O, true>(room, v, to, stride, rows, cols, f, wide);
+    else put_tile<O, false>(room, v, to, stride, rows, cols, f, wide);
 }
 
 // ---- the kernel ----------------------------------------------------------------------------------------------------------------

@@ -120,10 +120,9 @@ __global__ void __launch_bounds__(kGatherThreads) vocab_gather(const __grid_cons
         __syncthreads();
     }
     if (!last_block) return;
-    if (tid == 0) {
-        a.head->rows = base;
-        a.head->top = m;
-        a.head->parts = a.dloss ? parts_of((uint32_t)base, (uint32_t)a.D, (uint32_t)a.vocab_blocks, (uint32_t)a.pairs, a.acc_rows) : 1;
+    if (warp == 0) {
+        const int32_t parts = a.dloss ? parts_of((uint32_t)base, (uint32_t)a.D, (uint32_t)a.vocab_blocks, (uint32_t)a.pairs, a.acc_rows) : 1;
+        if (lane == 0) { a.head->rows = base; a.head->top = m; a.head->parts = parts; }
     }
     // dW is summed over whole blocks of kRowBlock rows: what follows the last row there is zero
     if (a.dloss) {
