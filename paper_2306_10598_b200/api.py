@@ -420,7 +420,7 @@ def _matrix(t: torch.Tensor, name: str, device: Optional[torch.device] = None, d
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     dt = t.dtype
-    if dt not in _DTYPE or (dtype is not None and dt != dtype):
+    if dt not in _DTYPE or (dtype is not None and dt is not dtype):
         raise TypeError(f"{name} must be {dtype or 'bfloat16, float16 or float32'}, got {dt}")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, not {device}")
@@ -438,12 +438,17 @@ def _matrix(t: torch.Tensor, name: str, device: Optional[torch.device] = None, d
 
 
 def _vector(t: torch.Tensor, name: str, dtype: torch.dtype, n: int, device: torch.device) -> int:
-    p = _dev(t, dtype, name)
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     if t.numel() != n:
         raise ValueError(f"{name} must hold {n} values, got {t.numel()}")
-    return p
+    return t.data_ptr()
 
 
 def _same(name: str, got, want) -> None:
@@ -464,10 +469,6 @@ def _call(device: torch.device, where: str, fn, *args) -> None:
             status = fn(*args, _raw_stream(index))
     if status:
         _check(status, where)
-
-
-def _workspace(ws: Optional[torch.Tensor], need: int, device: torch.device) -> torch.Tensor:
-    return torch.empty(need, dtype=torch.uint8, device=device) if ws is None else ws
 
 
 def dc_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, pad_id: int = -1) -> None:
@@ -562,11 +563,20 @@ def dc_train_status() -> int:
     return int(flags.value)
 
 
-# The same with outputs and workspaces allocated by torch.
+# The same with outputs and workspaces allocated by torch (what they allocate themselves is not checked again).
+
+def _bytes(n: int, device: torch.device) -> torch.Tensor:
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
 
 def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, pad_id: int = -1) -> torch.Tensor:
-    out = table.new_empty((*ids.shape, table.shape[-1]))
-    dc_embed(table, ids, out, scale, pad_id)
+    """scale * table[ids], of ids' shape and one dimension more."""
+    device, dt = table.device, table.dtype
+    t, ts, V, D = _matrix(table, "table")
+    N = ids.numel()
+    i = _vector(ids, "ids", torch.int64, N, device)
+    out = torch.empty((*ids.shape, D), dtype=dt, device=device)
+    _call(device, "dc_embed", _lib.dc_embed, t, ts, _DTYPE[dt], i, N, V, D, scale, pad_id, out.data_ptr(), D)
     return out
 
 
@@ -581,8 +591,9 @@ def embed_backward(dout: torch.Tensor, ids: torch.Tensor, V: int, scale: float =
         dtable = torch.empty((V, D), dtype=dtype or dout.dtype, device=dout.device)
     else:
         _same("dtable", dtable.shape, (V, D))
-    dc_embed_backward(dout, ids, dtable, _workspace(workspace, dc_embed_backward_workspace_bytes(ids.numel(), V, D), dout.device), scale,
-                      pad_id, accumulate)
+    if workspace is None:
+        workspace = _bytes(dc_embed_backward_workspace_bytes(ids.numel(), V, D), dout.device)
+    dc_embed_backward(dout, ids, dtable, workspace, scale, pad_id, accumulate)
     return dtable
 
 
@@ -593,18 +604,25 @@ class Saved8(NamedTuple):
 
 
 def gelu_save8(x: torch.Tensor) -> Saved8:
-    shape = x.shape
-    r = Saved8(x.new_empty(shape), x.new_empty(shape, dtype=torch.int8),
-               x.new_empty((*shape[:-1], -(-shape[-1] // SAVE8_GROUP)), dtype=torch.float32))
-    dc_gelu_save8(x, *r)
-    return r
+    device, dt, shape = x.device, x.dtype, x.shape
+    p, xs, N, D = _matrix(x, "x")
+    y = torch.empty(shape, dtype=dt, device=device)
+    q = torch.empty(shape, dtype=torch.int8, device=device)
+    scales = torch.empty((*shape[:-1], -(-D // SAVE8_GROUP)), dtype=torch.float32, device=device)
+    _call(device, "dc_gelu_save8", _lib.dc_gelu_save8, p, xs, _DTYPE[dt], N, D, y.data_ptr(), D, q.data_ptr(), scales.data_ptr())
+    return Saved8(y, q, scales)
 
 
 def gelu_save8_backward(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, want_y: bool = False):
     """dx, or (dx, y_again) with want_y."""
-    dx = dy.new_empty(dy.shape)
-    y = dy.new_empty(dy.shape) if want_y else None
-    dc_gelu_save8_backward(dy, q, scales, dx, y)
+    device, dt, shape = dy.device, dy.dtype, dy.shape
+    p, ds, N, D = _matrix(dy, "dy")
+    qp = _vector(q, "q", torch.int8, N * D, device)
+    sp = _vector(scales, "scales", torch.float32, N * -(-D // SAVE8_GROUP), device)
+    dx = torch.empty(shape, dtype=dt, device=device)
+    y = torch.empty(shape, dtype=dt, device=device) if want_y else None
+    _call(device, "dc_gelu_save8_backward", _lib.dc_gelu_save8_backward, p, ds, _DTYPE[dt], qp, sp, N, D, dx.data_ptr(), D,
+          y.data_ptr() if want_y else None, D)
     return (dx, y) if want_y else dx
 
 
@@ -615,10 +633,18 @@ class VocabLoss(NamedTuple):
 
 def vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100, logit_scale: float = 1.0,
                workspace: Optional[torch.Tensor] = None) -> VocabLoss:
-    loss = hidden.new_empty(targets.shape, dtype=torch.float32)
-    lse = hidden.new_empty(targets.shape, dtype=torch.float32)
-    dc_vocab_loss(hidden, weight, targets, loss, lse,
-                  _workspace(workspace, dc_vocab_loss_workspace_bytes(targets.numel(), weight, False), hidden.device), ignore_index, logit_scale)
+    device, shape = hidden.device, targets.shape
+    h, hs, N, D = _matrix(hidden, "hidden")
+    w, ws, V, Dw = _matrix(weight, "weight", device, hidden.dtype)
+    if Dw != D:
+        _same("weight", (V, Dw), (V, D))
+    t = _vector(targets, "targets", torch.int64, N, device)
+    loss = torch.empty(shape, dtype=torch.float32, device=device)
+    lse = torch.empty(shape, dtype=torch.float32, device=device)
+    if workspace is None:
+        workspace = _bytes(_lib.dc_vocab_loss_workspace_bytes(N, V, D, w, ws, 0), device)
+    _call(device, "dc_vocab_loss", _lib.dc_vocab_loss, h, hs, w, ws, _DTYPE[hidden.dtype], t, N, V, D, ignore_index, logit_scale,
+          loss.data_ptr(), lse.data_ptr(), _dev(workspace, torch.uint8, "workspace"), workspace.numel())
     return VocabLoss(loss, lse)
 
 
@@ -629,10 +655,11 @@ def vocab_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
     """(dhidden, dweight): dweight is a new tensor of the weight's type, or the given one (that type or fp32) written or added to."""
     if accumulate and dweight is None:
         raise ValueError("accumulate needs the dweight to add to")
-    dh = hidden.new_empty(hidden.shape) if want_dhidden else None
+    device = hidden.device
+    dh = torch.empty(hidden.shape, dtype=hidden.dtype, device=device) if want_dhidden else None
     if dweight is None and want_dweight:
-        dweight = weight.new_empty(weight.shape)
-    dc_vocab_loss_backward(hidden, weight, targets, lse, dloss, dh, dweight,
-                           _workspace(workspace, dc_vocab_loss_workspace_bytes(targets.numel(), weight, True), hidden.device),
-                           ignore_index, logit_scale, accumulate)
+        dweight = torch.empty(weight.shape, dtype=weight.dtype, device=device)
+    if workspace is None:
+        workspace = _bytes(dc_vocab_loss_workspace_bytes(targets.numel(), weight, True), device)
+    dc_vocab_loss_backward(hidden, weight, targets, lse, dloss, dh, dweight, workspace, ignore_index, logit_scale, accumulate)
     return dh, dweight

@@ -19,7 +19,8 @@ namespace dct {
 
 constexpr int kTileM = 256, kTileN = 256;   // rows and columns of a tile of the result
 constexpr int kRowBlock = 64;               // elements of the summed dimension to a stage of the ring
-constexpr int64_t kPieceBytes = int64_t(256) << 20;   // g of one piece of the vocabulary
+// g of one piece of the vocabulary.  8192 x 65536 x 1024 step, us: 64 MiB 4190, 128 MiB 4120, 256 MiB 4070, 512 MiB 3990, 1 GiB 3950
+constexpr int64_t kPieceBytes = int64_t(512) << 20;
 constexpr int kStageBytes = 2 * 128 * 64 * 2;
 constexpr int kTcThreads = 384;             // warp 0 copies, warp 1 multiplies, warp 2 has the tensor memory, warps 4-11 take tiles out
 constexpr int kMaxParts = 16;
@@ -337,8 +338,10 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
             float m = -INFINITY, s = 0.0f, at_label = 0.0f;
             const uint32_t from = tmem + buf * 256 + half * 128 + ((uint32_t)(quarter * 32) << 16);
             __syncwarp();
+            // rows that nothing is kept of are not taken out; g has zeros up to the next kRowBlock, which dW is summed over
+            const int32_t row0 = row - lane, rows_out = WHAT == kGrad ? (units.rows + kRowBlock - 1) / kRowBlock * kRowBlock : WHAT == kBack && t.dw ? p.V : units.rows;
 #pragma unroll 1
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < (row0 < rows_out ? 4 : 0); ++j) {
                 const int32_t col = c0 + j * 32;
                 float v[32];
                 if (t.blocks > 0) {
@@ -385,16 +388,15 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
                     }
                 } else {
                     float *room = reinterpret_cast<float *>(raw + (ring - smem_u32(raw)) + kStages * kStageBytes) + (warp - 4) * 32 * kPitch;
-                    const int32_t row0 = row - lane;
                     if (t.dw) {
                         const int32_t r = min(32, p.V - row0), c = p.D - col;
                         const int64_t at = (int64_t)row0 * p.dw_stride + col;
-                        if (r <= 0 || c <= 0) continue;
+                        if (c <= 0) break;
                         if (p.dw_f32) put_tile(room, v, (float *)p.dw + at, p.dw_stride, r, c, unscale, p.dw_add, p.dw_wide);
                         else put_tile(room, v, (T *)p.dw + at, p.dw_stride, r, c, unscale, p.dw_add, p.dw_wide);
                     } else {
                         const int32_t r = min(32, units.rows - row0);
-                        if (r <= 0 || col >= p.Dp || (t.blocks == 0 && !p.first)) continue;
+                        if (col >= p.Dp || (t.blocks == 0 && !p.first)) break;
                         put_tile(room, v, p.acc + ((int64_t)t.part * units.rows + row0) * p.Dp + col, p.Dp, r, 32, 1.0f, !p.first, true);
                     }
                 }

@@ -11,6 +11,7 @@
 // Rows without a label are taken out first (vocab_gather), so the products run over labelled rows alone and whatever the
 // others hold never meets a product.
 #include "train_common.cuh"
+#include "vocab_few.cuh"
 #include "vocab_gemm.cuh"
 
 namespace dct {
@@ -151,17 +152,8 @@ __global__ void __launch_bounds__(256) vocab_join(const Head *__restrict__ head,
     if (j >= head->rows) return;
     const float2 *p = part + j * tiles;
     float m = -INFINITY, s = 0.0f;                          // in powers of two, as the tiles are
-    auto add = [&](float om, float os) {
-        const float n = fmaxf(m, om);
-        // a maximum of -inf stands for a part without a finite logit; its sum is 0, or NaN if it holds one
-        s = (m == -INFINITY ? s : s * exp2_fast(m - n)) + (om == -INFINITY ? os : os * exp2_fast(om - n));
-        m = n;
-    };
-    for (int32_t t = lane; t < tiles; t += 32) add(p[t].x, p[t].y);
-    for (int d = 16; d; d >>= 1) {
-        const float om = __shfl_xor_sync(~0u, m, d), os = __shfl_xor_sync(~0u, s, d);
-        add(om, os);
-    }
+    for (int32_t t = lane; t < tiles; t += 32) join_parts(m, s, p[t].x, p[t].y);
+    for (int d = 16; d; d >>= 1) join_parts(m, s, __shfl_xor_sync(~0u, m, d), __shfl_xor_sync(~0u, s, d));
     if (lane == 0) {
         const float z = (m + log2f(s)) * 0.6931471805599453f;
         lse[row_of[j]] = z;
@@ -235,7 +227,8 @@ inline Plan make_plan(void *base, int64_t N, int64_t V, int64_t D, const void *w
     if (p.copy_weight) p.weight = take((size_t)V * p.Dp * 2);
     if (!backward) {
         p.hit = (float *)take(p.Lp * 4);
-        p.part = (float2 *)take((size_t)p.Lp * p.tiles_v * 16);
+        const size_t parts = (size_t)p.Lp * p.tiles_v * 2, of_few = (size_t)kFewTokens * kMostFewBlocks;
+        p.part = (float2 *)take((parts > of_few ? parts : of_few) * 8);
     } else {
         p.row_lse = (float *)take(p.Lp * 4);
         p.row_factor = (float *)take(p.Lp * 4);
@@ -287,9 +280,21 @@ int readable(const Plan &p, const Gather &g, const void **weight, int64_t *ws, c
 }
 
 template <class T>
+int forward_few(const Gather &g, const Plan &p, const void *weight, int64_t ws, float *loss, float *lse, cudaStream_t st)
+{
+    Few a{};
+    a.hidden = g.hidden; a.hs = g.hs; a.weight = weight; a.ws = ws; a.targets = g.targets; a.ignore = g.ignore; a.V = g.V;
+    a.N = (int32_t)g.N; a.D = g.D; a.pitch = few_pitch(g.D); a.scale = g.logit_scale * 1.4426950408889634f; a.part = p.part; a.hit = p.hit;
+    const int32_t blocks = few_blocks(g.V), tiles = few_tiles(g.N);
+    if (int e = tiles == 1 ? few_launch<T, 1>(a, blocks, st) : few_launch<T, 2>(a, blocks, st)) return e;
+    return launch(vocab_few_join, dim3((unsigned)ceil_div(g.N, 4)), 128, 0, st, g.targets, g.ignore, g.V, (int32_t)g.N, p.part, p.hit, blocks, loss, lse);
+}
+
+template <class T>
 int forward(Gather g, const Plan &p, const void *weight, int64_t ws, float *loss, float *lse, cudaStream_t st)
 {
     constexpr bool bf = is_bf16<T>();
+    if (few(g.N, g.D, g.hidden, g.hs, weight, ws)) return forward_few<T>(g, p, weight, ws, loss, lse, st);
     const int32_t pairs = pairs_on_device<T>();
     if (pairs == 0) return DC_ERR_CUDA;
     CUtensorMap a, b;

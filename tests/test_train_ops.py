@@ -294,7 +294,9 @@ def check_backward(api, h, w, t, dloss, lse, e, span, ignore=-100, c=1.0, dw_dty
 
 
 LOSS = [(1, 1, 1), (1, 2, 8), (2, 7, 64), (31, 255, 63), (32, 256, 64), (33, 257, 65), (64, 1000, 128), (65, 5003, 129), (127, 300, 200), (128, 512, 72),
-        (129, 513, 264), (255, 130, 1024), (256, 2048, 320), (257, 4097, 136), (600, 777, 96), (1025, 1500, 520), (9, 32000, 256), (300, 9, 1032)]
+        (129, 513, 264), (255, 130, 1024), (256, 2048, 320), (257, 4097, 136), (600, 777, 96), (1025, 1500, 520), (9, 32000, 256), (300, 9, 1032),
+        # few tokens: one pass over the weight, up to 16 of them and as long as their rows fit
+        (1, 5000, 1024), (3, 70001, 72), (5, 1000, 1032), (8, 17, 40), (16, 4097, 200), (17, 300, 520), (32, 5003, 1024), (15, 5003, 1024), (16, 40, 3080), (7, 100, 6152), (33, 1000, 1024)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
@@ -322,6 +324,23 @@ def test_vocab_loss_rows_without_a_label(api, keep, ignore, dtype):
     check_backward(api, h0, w, t, d0, lse, e, span, ignore)
     if keep == 0.0:
         assert bool((dw == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_vocab_loss_few_tokens_without_a_label(api, dtype):
+    for N in (1, 6, 20, 32):
+        h, w, t, _ = make_loss(N, 900, 264, dtype, N)
+        t[::3] = -100
+        h[::3] = NAN
+        if N > 4:
+            t[1], t[4] = 900, -7
+        loss, lse, _, _ = check_forward(api, h, w, t)
+        assert bool((loss[::3] == 0).all()) and bool((lse[::3] == 0).all())
+        hs, ws = spaced(h, 8), spaced(w, 8)
+        again = api.vocab_loss(hs, ws, t)
+        assert torch.equal(again.loss.nan_to_num(5.0), loss.nan_to_num(5.0)) and torch.equal(again.lse.nan_to_num(5.0), lse.nan_to_num(5.0))
+        t[:] = -100
+        assert bool((api.vocab_loss(h, w, t).loss == 0).all())
 
 
 def test_vocab_loss_targets_outside(api):
