@@ -8,7 +8,8 @@
 
 namespace dct {
 
-constexpr int kTile = 32;            // places of the grouped list per tile
+constexpr int kTile = 32;            // places of the grouped list per tile, one to a lane
+constexpr int kSumThreads = 64;
 constexpr int kBuckets = 128;        // blocks of embed_sort; more where a bucket would hold more than kMaxKeys tokens
 constexpr int kMaxKeys = 4096;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
     __shared__ uint16_t list_key[kList];
     __shared__ int32_t warp_mine[kSortWarps], warp_less[kSortWarps], warp_sum[kSortWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int32_t bucket = blockIdx.x, mask = gridDim.x - 1;
+    const uint32_t bucket = blockIdx.x, mask = gridDim.x - 1;
     const int32_t keys = (int32_t)((vocab + mask) >> log_buckets);
     for (int32_t k = tid; k < keys; k += kSortThreads) hist[k] = 0;
     __syncthreads();
@@ -81,46 +82,47 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
         for (int u = 0; u < U; ++u) id[u] = i0 + u * 32 + lane < hi ? ids[i0 + u * 32 + lane] : -1;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const bool ok = id[u] >= 0 && id[u] < vocab && id[u] != pad;
-            const int32_t b = (int32_t)id[u] & mask;
-            const bool is = ok && b == bucket;
-            const uint32_t all = __ballot_sync(~0u, is);
-            const int32_t s = mine + __popc(all & ((1u << lane) - 1));
-            if (is) {
-                atomicAdd(&hist[id[u] >> log_buckets], 1);
+            const uint64_t x = (uint64_t)id[u];
+            const uint32_t b = x < (uint64_t)vocab && x != (uint64_t)pad ? (uint32_t)x & mask : ~0u;
+            less += b < bucket;
+            const uint32_t all = __ballot_sync(~0u, b == bucket);
+            if (all == 0) continue;
+            if (b == bucket) {
+                const int32_t s = mine + __popc(all & ((1u << lane) - 1));
+                atomicAdd(&hist[x >> log_buckets], 1);
                 if (s < kWarpList) {                                              // kept at once, as long as each warp has room
                     list_place[warp * kWarpList + s] = (int32_t)(i0 + u * 32 + lane);
-                    list_key[warp * kWarpList + s] = (uint16_t)(id[u] >> log_buckets);
+                    list_key[warp * kWarpList + s] = (uint16_t)(x >> log_buckets);
                 }
             }
             mine += __popc(all);
-            less += ok && b < bucket;
         }
     }
     less = __reduce_add_sync(~0u, less);
     if (lane == 0) { warp_mine[warp] = mine; warp_less[warp] = less; }
     const bool kept = !__syncthreads_or(mine > kWarpList);
-    int32_t begin = 0, total = 0, first = 0;                                      // of this warp, of the bucket, of the bucket's part
-    for (int w = 0; w < kSortWarps; ++w) {
-        if (w == warp) begin = total;
-        total += warp_mine[w];
-        first += warp_less[w];
+    // of this warp, of the bucket, of the bucket's part: a lane has a warp's counts
+    int32_t upto = warp_mine[lane];
+    const int32_t first = __reduce_add_sync(~0u, warp_less[lane]), total = __reduce_add_sync(~0u, upto);
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t o = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += o;
     }
+    const int32_t begin = __shfl_sync(~0u, upto, warp) - mine;
     if (bucket == mask && tid == 0) *live = first + total;
 
     // exclusive sum over the tokens of the bucket: each thread a run of neighbours, then the warps' totals
     const int32_t run = (keys + kSortThreads - 1) / kSortThreads, k0 = tid * run, k1 = min(keys, k0 + run);
     int32_t own = 0;
     for (int32_t k = k0; k < k1; ++k) own += hist[k];
-    int32_t upto = own;
+    upto = own;
     for (int d = 1; d < 32; d <<= 1) {
         const int32_t o = __shfl_up_sync(~0u, upto, d);
         if (lane >= d) upto += o;
     }
     if (lane == 31) warp_sum[warp] = upto;
     __syncthreads();
-    int32_t at = upto - own;
-    for (int w = 0; w < warp; ++w) at += warp_sum[w];
+    int32_t at = upto - own + __reduce_add_sync(~0u, lane < warp ? warp_sum[lane] : 0);
     for (int32_t k = k0; k < k1; ++k) {
         const int32_t c = hist[k];
         hist[k] = at;
@@ -142,16 +144,37 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
             if (is) {
                 if (rank == 0) hist[key] = next + __popc(same);
                 place[first + next + rank] = list_place[from_list + j0 + lane];
-                token[first + next + rank] = (key << log_buckets) + bucket;
+                token[first + next + rank] = (key << log_buckets) + (int32_t)bucket;
             }
             __syncwarp();
         }
     };
-    // one warp after the other
+    // The same for all warps' parts of the list: only taking the tokens' next places has to go by turns.
     auto put_in_turn = [&](int32_t have) {
+        int32_t key[kWarpList / 32], next[kWarpList / 32];
+        uint32_t same[kWarpList / 32];
+#pragma unroll
+        for (int i = 0; i < kWarpList / 32; ++i) {
+            key[i] = i * 32 + lane < have ? list_key[warp * kWarpList + i * 32 + lane] : -1;
+            same[i] = __match_any_sync(~0u, key[i]);
+        }
         for (int w = 0; w < kSortWarps; ++w) {
-            if (w == warp) put(warp * kWarpList, have);
+            if (w == warp)
+#pragma unroll
+                for (int i = 0; i < kWarpList / 32; ++i) {
+                    const bool takes = key[i] >= 0 && (same[i] & ((1u << lane) - 1)) == 0;
+                    if (takes) { next[i] = hist[key[i]]; hist[key[i]] = next[i] + __popc(same[i]); }
+                    __syncwarp();
+                }
             __syncthreads();
+        }
+#pragma unroll
+        for (int i = 0; i < kWarpList / 32; ++i) {
+            const int32_t to = __shfl_sync(~0u, next[i], __ffs(same[i]) - 1) + first + __popc(same[i] & ((1u << lane) - 1));
+            if (key[i] >= 0) {
+                place[to] = list_place[warp * kWarpList + i * 32 + lane];
+                token[to] = (key[i] << log_buckets) + (int32_t)bucket;
+            }
         }
     };
     if (kept && total <= 1024) {
@@ -179,7 +202,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
             for (int64_t i0 = lo; i0 < hi; i0 += 32) {
                 const int64_t i = i0 + lane;
                 const int64_t id = i < hi ? ids[i] : -1;
-                const bool is = id >= 0 && id < vocab && id != pad && ((int32_t)id & mask) == bucket;
+                const bool is = id >= 0 && id < vocab && id != pad && ((uint32_t)id & mask) == bucket;
                 const uint32_t all = __ballot_sync(~0u, is);
                 const int32_t s = r + __popc(all & ((1u << lane) - 1)) - from;
                 if (is && s >= 0 && s < kList) { list_place[s] = (int32_t)i; list_key[s] = (uint16_t)(id >> log_buckets); }
@@ -187,6 +210,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
             }
         __syncthreads();
         put_in_turn(max(0, min(kWarpList, total - from - warp * kWarpList)));
+        __syncthreads();
     }
 }
 
@@ -217,93 +241,104 @@ template <class O, int V> __device__ __forceinline__ void finish_row(O *row, con
     *reinterpret_cast<Pack<O, V> *>(row) = o;
 }
 
-// A warp takes (tile, 32 V columns).  part[tile][0] is the sum of the places at the tile's start whose token began in an
-// earlier tile, part[tile][1] of those at its end whose token goes on in the next one.
+// A warp takes (tile, 32 V columns).  All rows of the tile are on their way to shared memory at once, a thread's own columns to
+// its own place, and are then added run by run.  (Held in registers instead, the unrolled code was bound by its own fetching:
+// 65536 tokens x 1024, bf16 to fp32, 106 us with 8 rows of 16 bytes on their way, 248 with 32 of 8 bytes.)
+// part[tile][0] is the sum of the places at the tile's start whose token began in an earlier tile, part[tile][1] of those at its
+// end whose token goes on in the next one.  Blocks from sum_blocks on write zeros to the rows of tokens that do not occur.
 template <class T, class O, int V>
-__global__ void __launch_bounds__(128) embed_sum(const T *__restrict__ dout, int64_t ds, const int32_t *__restrict__ place, const int32_t *__restrict__ token,
-                                                 const int32_t *__restrict__ live, int64_t D, float scale, O *__restrict__ dtable, int64_t ts, bool accumulate,
-                                                 float *__restrict__ part, int64_t pitch, int32_t chunks, int64_t sum_blocks, const uint8_t *__restrict__ occurs,
-                                                 int64_t vocab)
+__global__ void __launch_bounds__(kSumThreads) embed_sum(const T *__restrict__ dout, int64_t ds, const int32_t *__restrict__ place, const int32_t *__restrict__ token,
+                                                         const int32_t *__restrict__ live, int64_t D, float scale, O *__restrict__ dtable, int64_t ts,
+                                                         bool accumulate, float *__restrict__ part, int64_t pitch, int32_t chunks, int32_t N, int64_t sum_blocks,
+                                                         const uint8_t *__restrict__ occurs, int64_t vocab)
 {
-    constexpr int U = 8;                                   // rows on their way at a time
-    const int lane = threadIdx.x & 31;
+    constexpr int W = kSumThreads / 32;
+    __shared__ Pack<T, V> rows[W][kTile][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     follow();
     if (blockIdx.x >= sum_blocks) {
-        // rows of tokens that do not occur
-        const int64_t step = (int64_t)(gridDim.x - sum_blocks) * 4;
-        for (int64_t v = (blockIdx.x - sum_blocks) * 4 + (threadIdx.x >> 5); v < vocab; v += step) {
+        const int64_t step = (int64_t)(gridDim.x - sum_blocks) * W;
+        for (int64_t v = (blockIdx.x - sum_blocks) * W + warp; v < vocab; v += step) {
             if (occurs[v]) continue;
             const Pack<O, V> zero = {};
             for (int64_t c = lane * V; c < D; c += 32 * V) *reinterpret_cast<Pack<O, V> *>(dtable + v * ts + c) = zero;
         }
         return;
     }
-    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int64_t task = (int64_t)blockIdx.x * W + warp;
     const int64_t tile = task / chunks;
     const int64_t c = (task - tile * chunks) * (32 * V) + lane * V;
-    const int32_t n = *live;
-    const int64_t begin = tile * kTile;
+    const int64_t begin = tile * kTile, i = begin + lane;
+    // all that is needed of the list, whether it reaches as far or not: places and tokens have room for all N
+    const int32_t n = *live, my_place = i < N ? place[i] : 0, before = begin > 0 ? token[begin - 1] : -1;
+    int32_t my_token = i < N ? token[i] : -1, next = i + 1 < N ? token[i + 1] : -1;
     if (begin >= n) return;
+    if (i >= n) my_token = -1;
+    if (i + 1 >= n) next = -1;
     const int32_t m = (int32_t)min((int64_t)kTile, n - begin);
-    const int32_t my_place = lane < m ? place[begin + lane] : 0;
-    const int32_t my_token = lane < m ? token[begin + lane] : -1;
-    const int32_t before = begin > 0 ? token[begin - 1] : -1, after = begin + m < n ? token[begin + m] : -1;
-    float sum[V] = {};
-    int32_t run_from = 0;
-    for (int32_t j0 = 0; j0 < m; j0 += U) {
-        Pack<T, V> p[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t at = __shfl_sync(~0u, my_place, (j0 + u) & 31);
-            if (j0 + u < m && c < D) p[u] = *reinterpret_cast<const Pack<T, V> *>(dout + (int64_t)at * ds + c);
+    Pack<T, V> (*mine)[32] = rows[warp];
+    if constexpr (sizeof(Pack<T, V>) == 16) {
+#pragma unroll 8
+        for (int32_t j = 0; j < m; ++j) {
+            const int64_t at = __shfl_sync(~0u, my_place, j);
+            if (c < D)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&mine[j][lane])), "l"(dout + at * ds + c) : "memory");
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else {
+        for (int32_t j0 = 0; j0 < m; j0 += 8) {
+            Pack<T, V> x[8];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t j = j0 + u;
-            if (j >= m) break;
-            const int32_t tok = __shfl_sync(~0u, my_token, j);
-            const int32_t next = j + 1 < m ? __shfl_sync(~0u, my_token, (j + 1) & 31) : after;
-            if (c < D) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) sum[i] += to_f(p[u].v[i]);
+            for (int u = 0; u < 8; ++u) {
+                const int64_t at = __shfl_sync(~0u, my_place, (j0 + u) & 31);
+                if (j0 + u < m && c < D) x[u] = *reinterpret_cast<const Pack<T, V> *>(dout + at * ds + c);
             }
-            const bool ends = next != tok, last = j + 1 == m;
-            if (ends || last) {
-                const bool began_earlier = run_from == 0 && before == tok;
-                if (c < D) {
-                    if (ends && !began_earlier) {
-                        finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
-                    } else {
-                        float *to = part + (tile * 2 + (began_earlier ? 0 : 1)) * pitch + c;
 #pragma unroll
-                        for (int i = 0; i < V; ++i) to[i] = sum[i];
-                    }
-                }
+            for (int u = 0; u < 8; ++u)
+                if (j0 + u < m && c < D) mine[j0 + u][lane] = x[u];
+        }
+    }
+    const uint32_t ends = __ballot_sync(~0u, lane < m && next != my_token);
+    for (int32_t j0 = 0; j0 < m;) {
+        const uint32_t rest = ends >> j0;
+        const int32_t j1 = rest ? j0 + __ffs(rest) : m;
+        float sum[V] = {};
+#pragma unroll 4
+        for (int32_t j = j0; j < j1; ++j) {
+            const Pack<T, V> x = mine[j][lane];
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum[i] = 0.0f;
-                run_from = j + 1;
+            for (int i = 0; i < V; ++i) sum[i] += to_f(x.v[i]);
+        }
+        const int32_t tok = __shfl_sync(~0u, my_token, j0);
+        const bool began_earlier = j0 == 0 && before == tok;
+        if (c < D) {
+            if (rest && !began_earlier) {
+                finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
+            } else {
+                float *to = part + (tile * 2 + (began_earlier ? 0 : 1)) * pitch + c;
+#pragma unroll
+                for (int i = 0; i < V; ++i) to[i] = sum[i];
             }
         }
+        j0 = j1;
     }
 }
 
-// A token that begins in a tile and goes on in the next: its partial sums in the order of the tiles, a quarter of them to each
-// warp of the block.
+// A token that begins in a tile and goes on in the next: its partial sums in the order of the tiles, a quarter of them to
+// each quarter of the block, 128 V columns at a time.
 template <class O, int V>
-__global__ void __launch_bounds__(128) embed_join(const int32_t *__restrict__ token, const int32_t *__restrict__ live, int64_t D, float scale,
-                                                  O *__restrict__ dtable, int64_t ts, bool accumulate, const float *__restrict__ part, int64_t pitch)
+__global__ void __launch_bounds__(512) embed_join(const int32_t *__restrict__ token, const int32_t *__restrict__ live, int64_t D, float scale,
+                                                  O *__restrict__ dtable, int64_t ts, bool accumulate, const float *__restrict__ part, int64_t pitch, int32_t N)
 {
-    constexpr int U = 8;
-    __shared__ float quarter[4][V][32];
+    constexpr int U = V == 8 ? 4 : 8;
+    __shared__ float others[3][V][128];
     follow();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t tile = blockIdx.x;
-    const int32_t n = *live;
-    const int64_t end = (tile + 1) * kTile;
-    if (end >= n) return;                                                    // the last tile has nothing behind it
-    const int32_t tok = token[end - 1];
-    if (token[end] != tok) return;                                           // nothing goes on
-    if (tile > 0 && token[tile * kTile] == tok && token[tile * kTile - 1] == tok) return;   // it began in an earlier tile
+    const int lane = threadIdx.x & 31, at = threadIdx.x & 127, quarter = threadIdx.x >> 7;
+    const int64_t tile = blockIdx.x, begin = tile * kTile, end = begin + kTile;
+    if (end >= N) return;                                                    // the last tile has nothing behind it
+    const int32_t n = *live, tok = token[end - 1], behind = token[end], start = token[begin], before = begin > 0 ? token[begin - 1] : -1;
+    if (end >= n || behind != tok) return;                                   // nothing goes on
+    if (start == tok && before == tok) return;                               // it began in an earlier tile
     int64_t last = tile + 1;                                                 // the tile that it ends in
     for (;;) {
         const int64_t t = last + 1 + lane;
@@ -311,35 +346,34 @@ __global__ void __launch_bounds__(128) embed_join(const int32_t *__restrict__ to
         last += on == ~0u ? 32 : __ffs(~on) - 1;
         if (on != ~0u) break;
     }
-    const int64_t each = (last - tile + 3) / 4, t0 = tile + 1 + warp * each, t1 = min(last + 1, t0 + each);
-    const int64_t c = (int64_t)blockIdx.y * (32 * V) + lane * V;
-    float sum[V] = {};
-    if (c < D) {
-        if (warp == 0) {
+    // part[tile][1], part[tile + 1][0], ... part[last][0]
+    const int64_t each = (last - tile + 4) / 4, t0 = tile + quarter * each, t1 = min(last + 1, t0 + each);
+    for (int64_t c0 = 0; c0 < D; c0 += 128 * V) {
+        const int64_t c = c0 + at * V;
+        float sum[V] = {};
+        if (c < D)
+            for (int64_t t = t0; t < t1; t += U) {
+                Pack<float, V> x[U];
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] = part[(tile * 2 + 1) * pitch + c + i];
+                for (int u = 0; u < U; ++u)
+                    if (t + u < t1) x[u] = *reinterpret_cast<const Pack<float, V> *>(part + ((t + u) * 2 + (t + u == tile)) * pitch + c);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[i] += t + u < t1 ? x[u].v[i] : 0.0f;
+            }
+        if (quarter > 0)
+#pragma unroll
+            for (int i = 0; i < V; ++i) others[quarter - 1][i][at] = sum[i];
+        __syncthreads();
+        if (quarter == 0 && c < D) {
+#pragma unroll
+            for (int q = 0; q < 3; ++q)
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] += others[q][i][at];
+            finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
         }
-        for (int64_t t = t0; t < t1; t += U) {
-            float x[U][V];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < V; ++i) x[u][i] = t + u < t1 ? part[(t + u) * 2 * pitch + c + i] : 0.0f;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < V; ++i) sum[i] += x[u][i];
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) quarter[warp][i][lane] = sum[i];
-    __syncthreads();
-    if (warp == 0 && c < D) {
-#pragma unroll
-        for (int w = 1; w < 4; ++w)
-#pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] += quarter[w][i][lane];
-        finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
+        __syncthreads();
     }
 }
 
@@ -378,13 +412,14 @@ int backward_launch(const void *dout, int64_t ds, int64_t N, int64_t vocab, int6
                     cudaStream_t st)
 {
     const int32_t chunks = (int32_t)ceil_div(D, 32 * V);
-    const int64_t tiles = ceil_div(N, kTile), sums = ceil_div(tiles * chunks, 4);
-    int64_t zeros = accumulate ? 0 : ceil_div(vocab, 4);
+    constexpr int W = kSumThreads / 32;
+    const int64_t tiles = ceil_div(N, kTile), sums = ceil_div(tiles * chunks, W);
+    int64_t zeros = accumulate ? 0 : ceil_div(vocab, W);
     if (zeros > (int64_t)sm_count() * 16) zeros = (int64_t)sm_count() * 16;
-    if (sums + zeros > INT32_MAX || chunks > 65535) return DC_ERR_RANGE;
-    if (int e = launch(embed_sum<T, O, V>, dim3((unsigned)(sums + zeros)), 128, 0, st, (const T *)dout, ds, w.place, w.token, w.live, D, scale, (O *)dtable, ts,
-                       accumulate, w.part, w.pitch, chunks, sums, w.occurs, vocab)) return e;
-    return launch(embed_join<O, V>, dim3((unsigned)tiles, (unsigned)chunks), 128, 0, st, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch);
+    if (sums + zeros > INT32_MAX) return DC_ERR_RANGE;
+    if (int e = launch(embed_sum<T, O, V>, dim3((unsigned)(sums + zeros)), kSumThreads, 0, st, (const T *)dout, ds, w.place, w.token, w.live, D, scale,
+                       (O *)dtable, ts, accumulate, w.part, w.pitch, chunks, (int32_t)N, sums, w.occurs, vocab)) return e;
+    return launch(embed_join<O, V>, dim3((unsigned)tiles), 512, 0, st, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch, (int32_t)N);
 }
 
 template <class T, int V>
@@ -457,9 +492,9 @@ extern "C" int dc_embed_backward(const void *dout, int64_t dout_stride, int32_t 
     if (pad_id < 0) pad_id = INT64_MIN;
     if (int e = launch(embed_sort, dim3(1u << p.log_buckets), kSortThreads, (size_t)p.keys * 4, st, ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token,
                        w.live, accumulate ? nullptr : w.occurs)) return e;
-    // packs of V elements on both sides: 16 bytes of dout, and as many elements of dtable
+    // packs of 16 bytes of dout, and of as many elements of dtable
     const int W = 16 / eb;
-    const bool wide = D % W == 0 && rows_on(dout, dout_stride, eb, 16) && rows_on(dtable, dtable_stride, ob, (size_t)(W * ob));
+    const bool wide = D % W == 0 && rows_on(dout, dout_stride, eb, (size_t)(W * eb)) && rows_on(dtable, dtable_stride, ob, (size_t)(W * ob));
 #define DCT_SUM(T, O, V_) backward_launch<T, O, V_>(dout, dout_stride, N, V, D, scale, dtable, dtable_stride, accumulate != 0, w, st)
     if (dtype == DC_F32) return wide ? DCT_SUM(float, float, 4) : DCT_SUM(float, float, 1);
     if (dtype == DC_BF16) {
