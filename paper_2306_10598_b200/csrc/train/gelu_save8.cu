@@ -100,9 +100,10 @@ template <bool FLAT> struct Groups {
             dcol = gap * kGroup;
             return;
         }
-        row = first / per_row;                                 // the only divisions of a thread
+        // the only divisions of a thread, in 32 bits where they can be: they are a good part of its work otherwise
+        row = (first | per_row) >> 32 ? first / per_row : (int64_t)((uint32_t)first / (uint32_t)per_row);
         col = (first - row * per_row) * kGroup;
-        drow = gap / per_row;
+        drow = gap < per_row ? 0 : (uint32_t)gap / (uint32_t)per_row;
         dcol = (gap - drow * per_row) * kGroup;
         wrap = per_row * kGroup;
     }
