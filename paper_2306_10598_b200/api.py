@@ -9,6 +9,7 @@ same name, and raises :class:`DropComputeError` on a non-zero status.  There is 
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -480,6 +481,7 @@ def dc_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: f
           scale, pad_id, o, os_)
 
 
+@functools.lru_cache(maxsize=256)
 def dc_embed_backward_workspace_bytes(N: int, V: int, D: int) -> int:
     return int(_lib.dc_embed_backward_workspace_bytes(N, V, D))
 
@@ -517,9 +519,15 @@ def dc_gelu_save8_backward(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tens
           _vector(scales, "scales", torch.float32, N * -(-D // SAVE8_GROUP), dy.device), N, D, o, xs, r, rs)
 
 
+@functools.lru_cache(maxsize=256)
+def _loss_bytes(N: int, V: int, D: int, weight_at: int, stride_at: int, backward: bool) -> int:
+    """The weight's place and stride count modulo 16 bytes alone."""
+    return int(_lib.dc_vocab_loss_workspace_bytes(N, V, D, weight_at, stride_at, int(backward)))
+
+
 def dc_vocab_loss_workspace_bytes(N: int, weight: torch.Tensor, backward: bool) -> int:
     w, ws, V, D = _matrix(weight, "weight")
-    return int(_lib.dc_vocab_loss_workspace_bytes(N, V, D, w, ws, int(backward)))
+    return _loss_bytes(N, V, D, w & 15, ws & 7, bool(backward))
 
 
 def dc_vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
@@ -649,7 +657,7 @@ def vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor
     loss = _empty(shape, torch.float32, device)
     lse = _empty(shape, torch.float32, device)
     if workspace is None:
-        workspace = _bytes(_lib.dc_vocab_loss_workspace_bytes(N, V, D, w, ws, 0), device)
+        workspace = _bytes(_loss_bytes(N, V, D, w & 15, ws & 7, False), device)
     _call(device, "dc_vocab_loss", _lib.dc_vocab_loss, h, hs, w, ws, _DTYPE[hidden.dtype], t, N, V, D, ignore_index, logit_scale,
           loss.data_ptr(), lse.data_ptr(), _dev(workspace, torch.uint8, "workspace"), workspace.numel())
     return VocabLoss(loss, lse)

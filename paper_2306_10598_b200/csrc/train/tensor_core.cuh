@@ -44,20 +44,34 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 10000;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 
-// Every wait is bounded: 2^17 tries that may each park the thread for 10 us.  When one runs out it is recorded for
-// dc_train_status and the whole CTA gives up: later waits return at once, and the loops around them end.
-constexpr uint32_t kTries = 1u << 17;
+// Every wait is bounded: by a second, and by a number of tries should the clock stand still.  When one runs out it is recorded
+// for dc_train_status and the whole CTA gives up: later waits return at once, and the loops around them end.  A try parks the
+// thread for as long as the hardware sees fit; asked to park it for up to 10 us, it woke late (large steps 2.5 % slower).
+constexpr uint32_t kTries = 1u << 24;
+constexpr uint64_t kLongest = 1000000000;
+__device__ __forceinline__ uint64_t nanoseconds()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *gave_up, uint32_t what)
 {
-    for (uint32_t i = 0; i < kTries; ++i) {
+    if (bar_try(bar, parity)) return true;
+    uint64_t began = 0;
+    for (uint32_t i = 1; i < kTries; ++i) {
         if (bar_try(bar, parity)) return true;
         if (*gave_up) return false;
+        if ((i & 63) == 0) {
+            if (began == 0) began = nanoseconds();
+            else if (nanoseconds() - began > kLongest) break;
+        }
     }
     *gave_up = 1;
     atomicOr(&g_train_wait_expired, what);
