@@ -6,8 +6,8 @@
 // elements is free as long as both operands have the same one: thread t of a row's four takes elements 8t ... 8t + 7 of each
 // 32, which feed two instructions.  Maximum and sum of exp stay in registers over all rows of the vocabulary that a warp meets.
 // Bound by the weight's bytes: 8 tokens x 32000 x 1024 bf16 are 65.5 MB, 10 us at the copy rate.  Measured, this path / the
-// general one: 1 token 18.1 / 25.8 us, 8 tokens 19.3 / 26.2, 16 tokens 22.0 / 26.4, 32 tokens 28.9 / 27.2 (every block brings in
-// all tokens), hence the limit; 8 tokens x 151552 61 / 71 (5.1 TB/s).
+// general one: 1 token 17.9 / 25.8 us, 8 tokens 17.7 / 26.2, 16 tokens 20.0 / 26.4, and 32 tokens, which it was built for too,
+// 28.9 / 27.2 (every block brings in all tokens), hence the limit; 8 tokens x 128000 49 us (5.3 TB/s).
 #pragma once
 
 #include "tensor_core.cuh"
@@ -36,6 +36,14 @@ __device__ __forceinline__ void few_product(float (&c)[4], uint32_t a0, uint32_t
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// 16 bytes that are read once: the memory's whole 256 bytes come into L2, where the warp's next reads find them
+__device__ __forceinline__ uint4 read_once(const void *p)
+{
+    uint4 r;
+    asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+
 struct Few {
     const void *hidden; int64_t hs;
     const void *weight; int64_t ws;
@@ -56,7 +64,7 @@ __device__ __forceinline__ void join_parts(float &m, float &s, float om, float o
 template <class T, int NT>
 __global__ void __launch_bounds__(kFewThreads, 2) vocab_few(const __grid_constant__ Few a)
 {
-    constexpr int U = 4, W = kFewThreads / 32;                   // U times 32 elements of 16 rows on their way
+    constexpr int U = 8, W = kFewThreads / 32;                   // U times 32 elements of 16 rows on their way
     extern __shared__ __align__(16) uint8_t room[];
     __shared__ float2 of_warp[W][NT * 8];
     __shared__ int32_t label[NT * 8];
@@ -71,8 +79,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) vocab_few(const __grid_constan
             const int32_t k = k0 + u * 32 + t * 8;
             x[u] = y[u] = make_uint4(0, 0, 0, 0);
             if (k < a.D) {
-                if (v < a.V) x[u] = *reinterpret_cast<const uint4 *>(r0 + k);
-                if (v + 8 < a.V) y[u] = *reinterpret_cast<const uint4 *>(r1 + k);
+                if (v < a.V) x[u] = read_once(r0 + k);
+                if (v + 8 < a.V) y[u] = read_once(r1 + k);
             }
         }
     };
