@@ -141,6 +141,12 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
+// log sum exp with the label's logit `hit`, as the tensor cores formed it, replaced by `exact`
+__device__ __forceinline__ float with_label(float lse, float hit, float exact)
+{
+    return lse + log1pf(__expf(hit - lse) * expm1f(exact - hit));
+}
+
 // ---- host: a matrix for bulk tensor copies, in boxes of 64 elements x `box_rows` -------------------------------------------
 
 inline bool tensor_map(CUtensorMap *m, const void *base, bool bf16, int64_t cols, int64_t rows, int64_t stride, int box_rows)

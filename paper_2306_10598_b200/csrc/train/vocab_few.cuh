@@ -159,26 +159,37 @@ __global__ void __launch_bounds__(kFewThreads, 2) vocab_few(const __grid_constan
     }
 }
 
-// A warp per token: the blocks' parts joined; tokens without a label are written here.
-__global__ void __launch_bounds__(128) vocab_few_join(const int64_t *__restrict__ targets, int64_t ignore, int64_t V, int32_t N, const float2 *__restrict__ part,
-                                                      const float *__restrict__ hit, int32_t blocks, float *__restrict__ loss, float *__restrict__ lse)
+// A warp per token: the blocks' parts joined, and the label's logit in fp32; tokens without a label are written here.
+template <class T>
+__global__ void __launch_bounds__(128) vocab_few_join(const __grid_constant__ Few a, int32_t blocks, float *__restrict__ loss, float *__restrict__ lse)
 {
-    follow();
     const int lane = threadIdx.x & 31;
     const int32_t n = blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (n >= N) return;
-    const int64_t l = targets[n];
-    if (l == ignore || l < 0 || l >= V) {
-        if (lane == 0) loss[n] = lse[n] = l == ignore ? 0.0f : __uint_as_float(0x7fffffffu);
+    follow();
+    if (n >= a.N) return;
+    const int64_t l = a.targets[n];
+    if (l == a.ignore || l < 0 || l >= a.V) {
+        if (lane == 0) loss[n] = lse[n] = l == a.ignore ? 0.0f : __uint_as_float(0x7fffffffu);
         return;
     }
+    float exact = 0.0f;
+    for (int32_t d = lane * 8; d < a.D; d += 256) {
+        const Pack<T, 8> h = *reinterpret_cast<const Pack<T, 8> *>((const T *)a.hidden + n * a.hs + d);
+        const Pack<T, 8> w = *reinterpret_cast<const Pack<T, 8> *>((const T *)a.weight + l * a.ws + d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) exact = fmaf(to_f(h.v[i]), to_f(w.v[i]), exact);
+    }
     float m = -INFINITY, s = 0.0f;
-    for (int32_t b = lane; b < blocks; b += 32) join_parts(m, s, part[(int64_t)n * blocks + b].x, part[(int64_t)n * blocks + b].y);
-    for (int d = 16; d; d >>= 1) join_parts(m, s, __shfl_xor_sync(~0u, m, d), __shfl_xor_sync(~0u, s, d));
+    for (int32_t b = lane; b < blocks; b += 32) join_parts(m, s, a.part[(int64_t)n * blocks + b].x, a.part[(int64_t)n * blocks + b].y);
+    for (int d = 16; d; d >>= 1) {
+        exact += __shfl_xor_sync(~0u, exact, d);
+        join_parts(m, s, __shfl_xor_sync(~0u, m, d), __shfl_xor_sync(~0u, s, d));
+    }
     if (lane == 0) {
-        const float z = (m + log2f(s)) * 0.6931471805599453f;
+        exact *= a.scale * 0.6931471805599453f;
+        const float z = with_label((m + log2f(s)) * 0.6931471805599453f, a.hit[n], exact);
         lse[n] = z;
-        loss[n] = z - hit[n];
+        loss[n] = z - exact;
     }
 }
 

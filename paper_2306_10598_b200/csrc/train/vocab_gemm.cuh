@@ -72,7 +72,7 @@ struct Product {
     const int32_t *label;
     float scale;                    // logit_scale * log2(e): logits in powers of two
     float2 *part; float *hit; int32_t part_pitch;
-    const float *lse, *factor;      // of each row
+    const float *lse, *factor, *row_hit;   // of each row; row_hit is the label's logit in fp32
     float *rest;                    // what the label's g loses by rounding
     void *grad; int32_t piece;
     int32_t v0;                     // first of the piece
@@ -367,12 +367,12 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
                     for (int i = 0; i < 32; ++i) v[i] = exp2_fast(fmaf(v[i], p.scale, -lse2)) * f;
                     if (__any_sync(~0u, l >= 0 && l < 32)) {
                         float g = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            v[i] = l == i ? v[i] - f : v[i];
-                            g = l == i ? v[i] : g;
+                        if (l >= 0 && l < 32) {
+                            g = expm1f(p.row_hit[row] - p.lse[row]) * f;
+                            p.rest[row] = g - to_f(from_f<T>(g));
                         }
-                        if (l >= 0 && l < 32) p.rest[row] = g - to_f(from_f<T>(g));
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = l == i ? g : v[i];
                     }
                     if (__any_sync(~0u, valid < 32)) {
 #pragma unroll

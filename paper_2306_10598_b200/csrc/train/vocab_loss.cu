@@ -8,6 +8,10 @@
 // g lies in [-1, 1] whatever dloss is.  Its largest element in a row is the label's as a rule; what rounding takes from that
 // one is kept per row in fp32 and put back into dh, which leaves dh with little more than the rounding of the result.  dW keeps
 // it: each of its terms is off by the rounding of g, as if the result were rounded a second time.
+// The label's logit is also formed on its own, in fp32 (vocab_gather): the tensor cores cut off what does not fit at each of their
+// D / 16 additions, which takes about 1.5e-6 from a logit at D = 1024, always to the same side.  lse gets the difference of its
+// label's term, the loss is taken from that logit, and so is the label's g, as expm1: it keeps its digits where the label is
+// nearly certain.
 // Rows without a label are taken out first (vocab_gather), so the products run over labelled rows alone and whatever the
 // others hold never meets a product.
 #include "train_common.cuh"
@@ -27,7 +31,8 @@ struct Gather {
     int64_t N, V; int32_t D, Dp;
     int32_t per_block;                     // rows of a block, a multiple of 32
     float logit_scale;
-    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_factor;
+    const void *weight; int64_t ws;        // rows start on 16-byte boundaries
+    Head *head; int32_t *row_of, *pos_of, *label; float *row_hit, *row_lse, *row_factor;
     void *rows;                            // [Lp][Dp]
     float *loss_out, *lse_out;             // forward only: rows without a label are written here
     int32_t vocab_blocks, pairs; int64_t acc_rows;
@@ -102,21 +107,33 @@ __global__ void __launch_bounds__(kGatherThreads) vocab_gather(const __grid_cons
         for (int j = warp; j < 32; j += W) {
             const int32_t to = where[j];
             if (to < 0) continue;
-            const T *from = hidden + (i0 + j) * a.hs;
+            const T *from = hidden + (i0 + j) * a.hs, *at_label = (const T *)a.weight + a.targets[i0 + j] * a.ws;
+            float hit = 0.0f;
             for (int32_t d0 = lane * V; d0 < a.Dp; d0 += 32 * V * U) {
-                Pack<T, V> x[U];
+                Pack<T, V> x[U], w[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int32_t d = d0 + u * 32 * V;
-                    x[u] = Pack<T, V>{};
-                    if (d < a.D) x[u] = *reinterpret_cast<const Pack<T, V> *>(from + d);
+                    x[u] = w[u] = Pack<T, V>{};
+                    if (d < a.D) {
+                        x[u] = *reinterpret_cast<const Pack<T, V> *>(from + d);
+                        if (V > 1) w[u] = *reinterpret_cast<const Pack<T, V> *>(at_label + d);
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int32_t d = d0 + u * 32 * V;
                     if (d < a.Dp) *reinterpret_cast<Pack<T, V> *>(rows + (int64_t)to * a.Dp + d) = x[u];
+                    if (V > 1)
+#pragma unroll
+                        for (int k = 0; k < V; ++k) hit = fmaf(to_f(x[u].v[k]), to_f(w[u].v[k]), hit);
                 }
             }
+            if (V == 1)                                     // in the order of the packs, so that the sum has the same bits
+                for (int32_t d0 = lane * 8; d0 < a.D; d0 += 256)
+                    for (int32_t d = d0; d < min(d0 + 8, a.D); ++d) hit = fmaf(to_f(from[d]), to_f(at_label[d]), hit);
+            for (int d = 16; d; d >>= 1) hit += __shfl_xor_sync(~0u, hit, d);
+            if (lane == 0) a.row_hit[to] = hit * a.logit_scale;
         }
         __syncthreads();
     }
@@ -144,7 +161,8 @@ __global__ void __launch_bounds__(256) vocab_copy_weight(const T *__restrict__ w
 // ---- joining the tiles of the vocabulary: a warp per row --------------------------------------------------------------------
 
 __global__ void __launch_bounds__(256) vocab_join(const Head *__restrict__ head, const int32_t *__restrict__ row_of, const float2 *__restrict__ part,
-                                                  const float *__restrict__ hit, int32_t tiles, float *__restrict__ loss, float *__restrict__ lse)
+                                                  const float *__restrict__ hit, const float *__restrict__ row_hit, int32_t tiles, float *__restrict__ loss,
+                                                  float *__restrict__ lse)
 {
     const int lane = threadIdx.x & 31;
     const int64_t j = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
@@ -155,9 +173,9 @@ __global__ void __launch_bounds__(256) vocab_join(const Head *__restrict__ head,
     for (int32_t t = lane; t < tiles; t += 32) join_parts(m, s, p[t].x, p[t].y);
     for (int d = 16; d; d >>= 1) join_parts(m, s, __shfl_xor_sync(~0u, m, d), __shfl_xor_sync(~0u, s, d));
     if (lane == 0) {
-        const float z = (m + log2f(s)) * 0.6931471805599453f;
+        const float z = with_label((m + log2f(s)) * 0.6931471805599453f, hit[j], row_hit[j]);
         lse[row_of[j]] = z;
-        loss[row_of[j]] = z - hit[j];
+        loss[row_of[j]] = z - row_hit[j];
     }
 }
 
@@ -205,7 +223,7 @@ struct Plan {
     int32_t Dp, tiles_v, piece, pieces, vocab_blocks;   // piece: columns of the vocabulary that g holds at a time
     int64_t Lp, acc_rows;
     bool copy_weight;
-    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_factor, *rest, *hit; float2 *part; char *rows, *weight, *grad; float *acc;
+    Head *head; int32_t *row_of, *pos_of, *label; float *row_lse, *row_factor, *rest, *hit; float2 *part; char *rows, *weight, *grad; float *acc, *row_hit;
     size_t bytes;
 };
 
@@ -223,6 +241,7 @@ inline Plan make_plan(void *base, int64_t N, int64_t V, int64_t D, const void *w
     p.row_of = (int32_t *)take(p.Lp * 4);
     p.pos_of = (int32_t *)take(p.Lp * 4);
     p.label = (int32_t *)take(p.Lp * 4);
+    p.row_hit = (float *)take(p.Lp * 4);
     p.rows = take((size_t)p.Lp * p.Dp * 2);
     if (p.copy_weight) p.weight = take((size_t)V * p.Dp * 2);
     if (!backward) {
@@ -260,8 +279,9 @@ inline int check(const void *hidden, int64_t hs, const void *weight, int64_t ws,
 }
 
 template <class T>
-int gather(Gather &g, cudaStream_t st)
+int gather(Gather &g, const Plan &p, const void *weight, int64_t ws, cudaStream_t st)
 {
+    g.weight = weight; g.ws = ws; g.row_hit = p.row_hit;
     g.per_block = (int32_t)(ceil_div(ceil_div(g.N, kGatherBlocks), 32) * 32);
     const unsigned blocks = (unsigned)ceil_div(g.N, g.per_block);
     const bool wide = g.D % 8 == 0 && rows_on(g.hidden, g.hs, 2, 16);
@@ -287,7 +307,7 @@ int forward_few(const Gather &g, const Plan &p, const void *weight, int64_t ws, 
     a.N = (int32_t)g.N; a.D = g.D; a.pitch = few_pitch(g.D); a.scale = g.logit_scale * 1.4426950408889634f; a.part = p.part; a.hit = p.hit;
     const int32_t blocks = few_blocks(g.V), tiles = few_tiles(g.N);
     if (int e = tiles == 1 ? few_launch<T, 1>(a, blocks, st) : few_launch<T, 2>(a, blocks, st)) return e;
-    return launch(vocab_few_join, dim3((unsigned)ceil_div(g.N, 4)), 128, 0, st, g.targets, g.ignore, g.V, (int32_t)g.N, p.part, p.hit, blocks, loss, lse);
+    return launch(vocab_few_join<T>, dim3((unsigned)ceil_div(g.N, 4)), 128, 0, st, a, blocks, loss, lse);
 }
 
 template <class T>
@@ -301,12 +321,12 @@ int forward(Gather g, const Plan &p, const void *weight, int64_t ws, float *loss
     Product q{};
     if (!tensor_map(&a, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&b, p.copy_weight ? p.weight : weight, bf, g.D, g.V, p.copy_weight ? p.Dp : ws, 128))
         return DC_ERR_CUDA;
-    if (int e = gather<T>(g, st)) return e;
     if (int e = readable<T>(p, g, &weight, &ws, st)) return e;
+    if (int e = gather<T>(g, p, weight, ws, st)) return e;
     q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.part = p.part; q.hit = p.hit; q.part_pitch = 2 * p.tiles_v;
     q.V = (int32_t)g.V; q.D = g.D; q.Dp = p.Dp;
     if (int e = launch_units<T, kLoss>(p.Lp / kTileM * p.tiles_v, pairs, a, b, a, b, q, st)) return e;
-    return launch(vocab_join, dim3((unsigned)ceil_div(g.N, 8)), 256, 0, st, p.head, p.row_of, p.part, p.hit, 2 * p.tiles_v, loss, lse);
+    return launch(vocab_join, dim3((unsigned)ceil_div(g.N, 8)), 256, 0, st, p.head, p.row_of, p.part, p.hit, p.row_hit, 2 * p.tiles_v, loss, lse);
 }
 
 template <class T>
@@ -316,8 +336,8 @@ int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, 
     const int32_t pairs = pairs_on_device<T>();
     if (pairs == 0) return DC_ERR_CUDA;
     g.vocab_blocks = p.vocab_blocks; g.pairs = pairs; g.acc_rows = p.acc_rows;
-    if (int e = gather<T>(g, st)) return e;
     if (int e = readable<T>(p, g, &weight, &ws, st)) return e;
+    if (int e = gather<T>(g, p, weight, ws, st)) return e;
     const int ob = dw_f32 ? 4 : 2;
     CUtensorMap rows, rows_mn, grad_k, grad_mn;
     if (!tensor_map(&rows, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&grad_k, p.grad, bf, p.piece, p.Lp, p.piece, 128) ||
@@ -330,7 +350,7 @@ int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, 
         CUtensorMap w_k, w_mn;
         if (!tensor_map(&w_k, w, bf, g.D, nv, ws, 128) || !tensor_map(&w_mn, w, bf, g.D, nv, ws, 64)) return DC_ERR_CUDA;
         Product q{};
-        q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.lse = p.row_lse; q.factor = p.row_factor; q.rest = p.rest; q.grad = p.grad; q.piece = p.piece;
+        q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.lse = p.row_lse; q.factor = p.row_factor; q.row_hit = p.row_hit; q.rest = p.rest; q.grad = p.grad; q.piece = p.piece;
         q.v0 = (int32_t)v0; q.V = (int32_t)nv; q.D = g.D; q.Dp = p.Dp; q.grad_scale = grad_scale<T>();
         if (int e = launch_units<T, kGrad>(tm * ceil_div(nv, kTileN), pairs, rows, w_k, rows, w_k, q, st)) return e;
         if (dw) {
