@@ -27,6 +27,7 @@ __global__ void __launch_bounds__(256) embed_kernel(const T *__restrict__ table,
     const int lane = threadIdx.x & 31;
     const int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int64_t n = task / chunks;
+    follow();
     if (n >= N) return;
     const int64_t c0 = (task - n * chunks) * (U * 32 * V) + lane * V;
     const int64_t id = ids[n];
@@ -466,8 +467,7 @@ int lookup(const void *table, int64_t ts, const int64_t *ids, int64_t N, int64_t
     const int32_t chunks = (int32_t)ceil_div(D, packs_of(V) * 32 * V);
     const int64_t blocks = ceil_div(N * chunks, 8);
     if (blocks > INT32_MAX) return DC_ERR_RANGE;
-    embed_kernel<T, V><<<(unsigned)blocks, 256, 0, st>>>((const T *)table, ts, ids, N, vocab, D, scale, pad, (T *)out, os, chunks);
-    return launched();
+    return launch(embed_kernel<T, V>, dim3((unsigned)blocks), 256, 0, st, (const T *)table, ts, ids, N, vocab, D, scale, pad, (T *)out, os, chunks);
 }
 
 inline int check(int64_t N, int64_t V, int64_t D, int32_t dtype)

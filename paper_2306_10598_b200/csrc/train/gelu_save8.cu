@@ -125,6 +125,7 @@ __global__ void __launch_bounds__(kThreads) gelu_save8_kernel(const T *__restric
     const int lane = threadIdx.x % H::LPG;
     const int64_t per_row = (D + kGroup - 1) / kGroup, first = (int64_t)blockIdx.x * H::PER + threadIdx.x / H::LPG;
     Groups<FLAT> g(first, H::GAP, per_row, D);
+    follow();
     Pack<T, V> p[kAhead][H::K];
     int64_t row[kAhead], col[kAhead];
 #pragma unroll
@@ -184,6 +185,7 @@ __global__ void __launch_bounds__(kThreads) gelu_save8_backward_kernel(const T *
     const int lane = threadIdx.x % H::LPG;
     const int64_t per_row = (D + kGroup - 1) / kGroup, first = (int64_t)blockIdx.x * H::PER + threadIdx.x / H::LPG;
     Groups<FLAT> g(first, H::GAP, per_row, D);
+    follow();
     Pack<T, V> p[kAhead][H::K];
     Bytes<V> b[kAhead][H::K];
     float scale[kAhead];
@@ -253,9 +255,8 @@ int forward(const void *x, int64_t xs, int64_t N, int64_t D, void *y, int64_t ys
     unsigned blocks;
     const bool flat = flatten(N, D, V > 1 && xs == D && ys == D);
     if (!blocks_for<Hold<T, V, kAheadForward>>(N, D, blocks)) return DC_ERR_RANGE;
-    if (flat) gelu_save8_kernel<T, V, V != 1><<<blocks, kThreads, 0, st>>>((const T *)x, xs, N, D, (T *)y, ys, q, scales);
-    else gelu_save8_kernel<T, V, false><<<blocks, kThreads, 0, st>>>((const T *)x, xs, N, D, (T *)y, ys, q, scales);
-    return launched();
+    return launch(flat ? gelu_save8_kernel<T, V, V != 1> : gelu_save8_kernel<T, V, false>, dim3(blocks), kThreads, 0, st, (const T *)x, xs, N, D, (T *)y, ys, q,
+                  scales);
 }
 template <class T, int V>
 int backward(const void *dy, int64_t dys, const int8_t *q, const float *scales, int64_t N, int64_t D, void *dx, int64_t dxs, void *y, int64_t ys,
@@ -264,9 +265,8 @@ int backward(const void *dy, int64_t dys, const int8_t *q, const float *scales, 
     unsigned blocks;
     const bool flat = flatten(N, D, V > 1 && dys == D && dxs == D && (!y || ys == D));
     if (!blocks_for<Hold<T, V, kAheadBackward>>(N, D, blocks)) return DC_ERR_RANGE;
-    if (flat) gelu_save8_backward_kernel<T, V, V != 1><<<blocks, kThreads, 0, st>>>((const T *)dy, dys, q, scales, N, D, (T *)dx, dxs, (T *)y, ys);
-    else gelu_save8_backward_kernel<T, V, false><<<blocks, kThreads, 0, st>>>((const T *)dy, dys, q, scales, N, D, (T *)dx, dxs, (T *)y, ys);
-    return launched();
+    return launch(flat ? gelu_save8_backward_kernel<T, V, V != 1> : gelu_save8_backward_kernel<T, V, false>, dim3(blocks), kThreads, 0, st, (const T *)dy, dys, q,
+                  scales, N, D, (T *)dx, dxs, (T *)y, ys);
 }
 
 }  // namespace dct

@@ -28,7 +28,6 @@ inline int sm_count()
     return n;
 }
 
-inline int launched() { return cudaGetLastError() == cudaSuccess ? DC_OK : DC_ERR_CUDA; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int elem_bytes(int32_t dtype) { return dtype == DC_F32 ? 4 : 2; }
@@ -36,7 +35,7 @@ inline bool on(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p)
 // rows of a matrix whose starts all fall on `a`-byte boundaries
 inline bool rows_on(const void *p, int64_t stride, int eb, size_t a) { return on(p, a) && (size_t)(stride * eb) % a == 0; }
 
-// Kernels of one call follow each other with programmatic dependent launch: the next one may start, and set itself up, while
+// Kernels follow each other, those of one call and of calls in a row, with programmatic dependent launch: the next one may start, and set itself up, while
 // the last blocks of the one before still run, and waits in follow() until that one is done and its writes are visible.  Every
 // kernel calls it before it touches global memory, so all that went before in the stream is done too.
 template <class... P, class... A> int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args)
