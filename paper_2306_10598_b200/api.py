@@ -429,7 +429,10 @@ def _matrix(t: torch.Tensor, name: str, device: Optional[torch.device] = None, d
     if len(shape) != 2:
         if not shape:
             raise ValueError(f"{name} must have at least one dimension")
-        t = t.view(-1, shape[-1]) if t.numel() else t.reshape(0, shape[-1])
+        try:
+            t = t.view(-1, shape[-1]) if t.numel() else t.reshape(0, shape[-1])
+        except RuntimeError:
+            raise ValueError(f"the rows of {name} must be evenly spaced") from None
         shape = t.shape
     rows, cols = shape
     stride, step = t.stride()

@@ -9,13 +9,15 @@ from . import api
 
 
 def _rows(t: torch.Tensor) -> torch.Tensor:
-    """A gradient as the library takes it: those of a sum or a mean are one value seen many times."""
+    """A tensor as the library takes it: gradients of a sum or a mean are one value seen many times, and the rows of a slice
+    of sequences need not be evenly spaced."""
     return t.contiguous()
 
 
 class _Embed(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, ids, scale, pad_id):
+        ids = _rows(ids)
         ctx.save_for_backward(ids)
         ctx.rest = (table.shape[0], scale, pad_id)
         return api.embed(table, ids, scale, pad_id)
@@ -30,7 +32,7 @@ class _Embed(torch.autograd.Function):
 class _Gelu(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x):
-        y, q, scales = api.gelu_save8(x)
+        y, q, scales = api.gelu_save8(_rows(x))
         ctx.save_for_backward(q, scales)
         return y
 
@@ -42,6 +44,7 @@ class _Gelu(torch.autograd.Function):
 class _VocabLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, targets, ignore_index, logit_scale):
+        hidden, targets = _rows(hidden), _rows(targets)
         loss, lse = api.vocab_loss(hidden, weight, targets, ignore_index, logit_scale)
         ctx.save_for_backward(hidden, weight, targets, lse)
         ctx.rest = (ignore_index, logit_scale)

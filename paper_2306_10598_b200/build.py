@@ -66,7 +66,8 @@ def _units():
     shared = [f for f in _train_sources() if f.endswith(".cuh")]
     for f in _train_sources():
         if f.endswith(".cu"):
-            yield f, ["-I", TRAIN], (f, *shared, HDRS[0], HDRS[2])
+            # without unique symbols: a second copy of the library in one process keeps what it knows of its own kernels to itself
+            yield f, ["-Xcompiler", "-fno-gnu-unique", "-I", TRAIN], (f, *shared, HDRS[0], HDRS[2])
 
 
 def _compile(src: str, flags: list, made_from: tuple, force: bool, verbose: bool):

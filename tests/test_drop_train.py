@@ -95,6 +95,11 @@ def test_differentiable_functions(mods):
     dy, dw = api.vocab_loss_backward(s.y, head.detach(), t, lse, torch.full_like(l, 1.0 / 36))
     dx = api.gelu_save8_backward(dy, s.q, s.scales)
     assert torch.equal(head.grad, dw) and torch.equal(table.grad, api.embed_backward(dx, ids, 50, 3.0, 7))
+    # sequences without their last place, as next-token training slices them
+    x2 = ag.gelu(ag.embed(table, ids[:, :-1], 3.0, 7))
+    shifted = ag.vocab_loss(ag.gelu(ag.embed(table, ids, 3.0, 7))[:, :-1], head, t[:, 1:])
+    assert torch.equal(shifted, ag.vocab_loss(x2, head, t[:, 1:].contiguous()))
+    shifted.sum().backward()
     # a head that is not trained costs no gradient of its own
     frozen = ag.vocab_loss(y.detach().requires_grad_(), head.detach(), t)
     frozen.sum().backward()

@@ -474,6 +474,43 @@ def test_on_another_stream(api):
     assert torch.equal(got[3].q, want[3].q) and torch.equal(back[0], grads[0]) and torch.equal(back[1], grads[1])
 
 
+def test_offsets_beyond_32_bits(api):
+    """Matrices of more than 2^31 elements: the last rows are what they would be alone."""
+    g = gen(40)
+    D = 2048
+    N = (1 << 31) // D + 300
+    table = normal(g, 70, D, dtype=BF16)
+    ids = torch.randint(0, 70, (N,), generator=g, device="cuda")
+    out = api.embed(table, ids, scale=2.0)
+    assert torch.equal(out[-300:], api.embed(table, ids[-300:], scale=2.0))
+    y, q, s = api.gelu_save8(out)
+    y1, q1, s1 = api.gelu_save8(out[-300:].clone())
+    assert torch.equal(y[-300:], y1) and torch.equal(q[-300:], q1) and torch.equal(s[-300:], s1)
+    dx = api.gelu_save8_backward(out, q, s)
+    assert torch.equal(dx[-300:], api.gelu_save8_backward(out[-300:].clone(), q1, s1))
+    del y, q, s, dx
+    # rows of the last places alone: the same loss; labels elsewhere are missing, so the gradients are theirs too
+    w = normal(g, 300, D, dtype=BF16, scale=0.02)
+    t = torch.full((N,), -100, device="cuda")
+    t[-300:] = torch.randint(0, 300, (300,), generator=g, device="cuda")
+    dloss = torch.full((N,), 1.0 / 300, device="cuda")
+    loss, lse = api.vocab_loss(out, w, t)
+    alone = api.vocab_loss(out[-300:].clone(), w, t[-300:].clone())
+    assert torch.equal(loss[-300:], alone.loss) and bool((loss[:-300] == 0).all())
+    dh, dw = api.vocab_loss_backward(out, w, t, lse, dloss)
+    dh1, dw1 = api.vocab_loss_backward(out[-300:].clone(), w, t[-300:].clone(), alone.lse, dloss[-300:].clone())
+    assert torch.equal(dw, dw1) and bool((dh[:-300] == 0).all())
+    rel = float((dh[-300:].float() - dh1.float()).norm() / dh1.float().norm())      # the vocabulary may be cut in other parts
+    assert rel <= 2.0 ** -8
+    del out, dh
+    # a table of more than 2^31 elements
+    V = (1 << 31) // 1024 + 50
+    d = normal(g, 64, 1024)
+    at = torch.randint(V - 40, V, (64,), generator=g, device="cuda")
+    grad = api.embed_backward(d, at, V)
+    assert torch.equal(grad[-40:], api.embed_backward(d, at - (V - 40), 40)) and bool((grad[:100] == 0).all()) and bool((grad[-60:-40] == 0).all())
+
+
 def test_refusals(api):
     h, w, t, dloss = make_loss(8, 50, 64, BF16, 5)
     f = torch.zeros(8, device="cuda")
@@ -489,6 +526,8 @@ def test_refusals(api):
         api.vocab_loss(h, w, t[:5])
     with pytest.raises(ValueError):
         api.vocab_loss(h, w.t().contiguous().t(), t)          # elements of a row apart
+    with pytest.raises(ValueError):
+        api.vocab_loss(h.view(2, 4, 64)[:, :3], w, t[:6])     # rows not evenly spaced
     with pytest.raises(api.DropComputeError) as x:
         api.vocab_loss(h.float(), w.float(), t)
     assert x.value.status == 7
