@@ -9,7 +9,6 @@ same name, and raises :class:`DropComputeError` on a non-zero status.  There is 
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -45,9 +44,10 @@ class DropComputeError(RuntimeError):
         super().__init__(f"{where}: status {status} ({status_string(status)})")
 
 
-if not os.path.exists(LIB_PATH):
+CALLS_PATH = os.path.join(_PKG, "_calls.so")   # the training operators' calls (see the end of this module)
+if not os.path.exists(LIB_PATH) or not os.path.exists(CALLS_PATH):
     raise ImportError(
-        f"{LIB_PATH} is missing: build it with `python -m paper_2306_10598_b200.build` "
+        f"{LIB_PATH if not os.path.exists(LIB_PATH) else CALLS_PATH} is missing: build it with `python -m paper_2306_10598_b200.build` "
         "(there is no CPU or PyTorch fallback for this library)")
 
 _lib = ctypes.CDLL(LIB_PATH)
@@ -460,19 +460,10 @@ def _same(name: str, got, want) -> None:
         raise ValueError(f"{name} must be {tuple(want)}, got {tuple(got)}")
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream   # current_stream(device).cuda_stream without the Stream object (2 us a call)
-
-
 def _call(device: torch.device, where: str, fn, *args) -> None:
     """Calls `fn(*args, stream)` with `device` current."""
-    index = device.index
-    if index == torch.cuda.current_device():
-        status = fn(*args, _raw_stream(index))
-    else:
-        with torch.cuda.device(device):
-            status = fn(*args, _raw_stream(index))
-    if status:
-        _check(status, where)
+    with torch.cuda.device(device):
+        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream), where)
 
 
 def dc_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, pad_id: int = -1) -> None:
@@ -484,7 +475,6 @@ def dc_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: f
           scale, pad_id, o, os_)
 
 
-@functools.lru_cache(maxsize=256)
 def dc_embed_backward_workspace_bytes(N: int, V: int, D: int) -> int:
     return int(_lib.dc_embed_backward_workspace_bytes(N, V, D))
 
@@ -522,15 +512,9 @@ def dc_gelu_save8_backward(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tens
           _vector(scales, "scales", torch.float32, N * -(-D // SAVE8_GROUP), dy.device), N, D, o, xs, r, rs)
 
 
-@functools.lru_cache(maxsize=256)
-def _loss_bytes(N: int, V: int, D: int, weight_at: int, stride_at: int, backward: bool) -> int:
-    """The weight's place and stride count modulo 16 bytes alone."""
-    return int(_lib.dc_vocab_loss_workspace_bytes(N, V, D, weight_at, stride_at, int(backward)))
-
-
 def dc_vocab_loss_workspace_bytes(N: int, weight: torch.Tensor, backward: bool) -> int:
     w, ws, V, D = _matrix(weight, "weight")
-    return _loss_bytes(N, V, D, w & 15, ws & 7, bool(backward))
+    return int(_lib.dc_vocab_loss_workspace_bytes(N, V, D, w, ws, int(backward)))
 
 
 def dc_vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
@@ -574,45 +558,24 @@ def dc_train_status() -> int:
     return int(flags.value)
 
 
-# The same with outputs and workspaces allocated by torch (what they allocate themselves is not checked again).
+# The same with outputs and workspaces allocated by torch, checked and called by the extension module beside the library
+# (the checks are those of the functions above).
 
-def _empty(shape, dtype: torch.dtype, device: torch.device) -> torch.Tensor:
-    """torch.empty; for a matrix with its strides given, which is 0.8 us quicker."""
-    if len(shape) == 2:
-        return torch.empty_strided(shape, (max(1, shape[1]), 1), dtype=dtype, device=device)
-    return torch.empty(shape, dtype=dtype, device=device)
+from . import _calls  # noqa: E402  (the library is loaded first)
 
-
-def _bytes(n: int, device: torch.device) -> torch.Tensor:
-    return torch.empty(n, dtype=torch.uint8, device=device)
+_calls.raise_with(DropComputeError)
 
 
 def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, pad_id: int = -1) -> torch.Tensor:
     """scale * table[ids], of ids' shape and one dimension more."""
-    device, dt = table.device, table.dtype
-    t, ts, V, D = _matrix(table, "table")
-    N = ids.numel()
-    i = _vector(ids, "ids", torch.int64, N, device)
-    out = _empty((*ids.shape, D), dt, device)
-    _call(device, "dc_embed", _lib.dc_embed, t, ts, _DTYPE[dt], i, N, V, D, scale, pad_id, out.data_ptr(), D)
-    return out
+    return _calls.embed(table, ids, scale, pad_id)
 
 
 def embed_backward(dout: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0, pad_id: int = -1,
                    dtable: Optional[torch.Tensor] = None, accumulate: bool = False, dtype: Optional[torch.dtype] = None,
                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The table's gradient [V, D]: a new tensor of `dtype` (dout's by default), or `dtable` written or added to."""
-    D = dout.shape[-1]
-    if dtable is None:
-        if accumulate:
-            raise ValueError("accumulate needs the dtable to add to")
-        dtable = _empty((V, D), dtype or dout.dtype, dout.device)
-    else:
-        _same("dtable", dtable.shape, (V, D))
-    if workspace is None:
-        workspace = _bytes(dc_embed_backward_workspace_bytes(ids.numel(), V, D), dout.device)
-    dc_embed_backward(dout, ids, dtable, workspace, scale, pad_id, accumulate)
-    return dtable
+    return _calls.embed_backward(dout, ids, V, scale, pad_id, dtable, accumulate, -1 if dtype is None else _DTYPE[dtype], workspace)
 
 
 class Saved8(NamedTuple):
@@ -622,26 +585,12 @@ class Saved8(NamedTuple):
 
 
 def gelu_save8(x: torch.Tensor) -> Saved8:
-    device, dt, shape = x.device, x.dtype, x.shape
-    p, xs, N, D = _matrix(x, "x")
-    y = _empty(shape, dt, device)
-    q = _empty(shape, torch.int8, device)
-    scales = _empty((*shape[:-1], -(-D // SAVE8_GROUP)), torch.float32, device)
-    _call(device, "dc_gelu_save8", _lib.dc_gelu_save8, p, xs, _DTYPE[dt], N, D, y.data_ptr(), D, q.data_ptr(), scales.data_ptr())
-    return Saved8(y, q, scales)
+    return Saved8._make(_calls.gelu_save8(x))
 
 
 def gelu_save8_backward(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, want_y: bool = False):
     """dx, or (dx, y_again) with want_y."""
-    device, dt, shape = dy.device, dy.dtype, dy.shape
-    p, ds, N, D = _matrix(dy, "dy")
-    qp = _vector(q, "q", torch.int8, N * D, device)
-    sp = _vector(scales, "scales", torch.float32, N * -(-D // SAVE8_GROUP), device)
-    dx = _empty(shape, dt, device)
-    y = _empty(shape, dt, device) if want_y else None
-    _call(device, "dc_gelu_save8_backward", _lib.dc_gelu_save8_backward, p, ds, _DTYPE[dt], qp, sp, N, D, dx.data_ptr(), D,
-          y.data_ptr() if want_y else None, D)
-    return (dx, y) if want_y else dx
+    return _calls.gelu_save8_backward(dy, q, scales, want_y)
 
 
 class VocabLoss(NamedTuple):
@@ -651,19 +600,7 @@ class VocabLoss(NamedTuple):
 
 def vocab_loss(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100, logit_scale: float = 1.0,
                workspace: Optional[torch.Tensor] = None) -> VocabLoss:
-    device, shape = hidden.device, targets.shape
-    h, hs, N, D = _matrix(hidden, "hidden")
-    w, ws, V, Dw = _matrix(weight, "weight", device, hidden.dtype)
-    if Dw != D:
-        _same("weight", (V, Dw), (V, D))
-    t = _vector(targets, "targets", torch.int64, N, device)
-    loss = _empty(shape, torch.float32, device)
-    lse = _empty(shape, torch.float32, device)
-    if workspace is None:
-        workspace = _bytes(_loss_bytes(N, V, D, w & 15, ws & 7, False), device)
-    _call(device, "dc_vocab_loss", _lib.dc_vocab_loss, h, hs, w, ws, _DTYPE[hidden.dtype], t, N, V, D, ignore_index, logit_scale,
-          loss.data_ptr(), lse.data_ptr(), _dev(workspace, torch.uint8, "workspace"), workspace.numel())
-    return VocabLoss(loss, lse)
+    return VocabLoss._make(_calls.vocab_loss(hidden, weight, targets, ignore_index, logit_scale, workspace))
 
 
 def vocab_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
@@ -671,13 +608,5 @@ def vocab_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, targets: tor
                         accumulate: bool = False, want_dhidden: bool = True, want_dweight: bool = True,
                         workspace: Optional[torch.Tensor] = None):
     """(dhidden, dweight): dweight is a new tensor of the weight's type, or the given one (that type or fp32) written or added to."""
-    if accumulate and dweight is None:
-        raise ValueError("accumulate needs the dweight to add to")
-    device = hidden.device
-    dh = _empty(hidden.shape, hidden.dtype, device) if want_dhidden else None
-    if dweight is None and want_dweight:
-        dweight = _empty(weight.shape, weight.dtype, device)
-    if workspace is None:
-        workspace = _bytes(dc_vocab_loss_workspace_bytes(targets.numel(), weight, True), device)
-    dc_vocab_loss_backward(hidden, weight, targets, lse, dloss, dh, dweight, workspace, ignore_index, logit_scale, accumulate)
-    return dh, dweight
+    return _calls.vocab_loss_backward(hidden, weight, targets, lse, dloss, ignore_index, logit_scale, dweight, accumulate, want_dhidden,
+                                      want_dweight, workspace)

@@ -1,7 +1,8 @@
 """Builds libdropcompute.so (the C-ABI library) in-tree with nvcc for sm_100a.
 
 One object per translation unit -- the sweep (csrc/dropcompute.cu) and each training operator (csrc/train/*.cu) -- compiled
-side by side and linked into one library.  Objects are kept in _build/ under a hash of what they were made from, so a change
+side by side and linked into one library; and the extension module through which api.py calls the training operators
+(csrc/train/calls.cpp, g++ against torch's headers).  Objects are kept in _build/ under a hash of what they were made from, so a change
 to one operator does not compile the sweep again."""
 from __future__ import annotations
 
@@ -9,6 +10,7 @@ import hashlib
 import os
 import shutil
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +20,7 @@ TRAIN = os.path.join(PKG, "csrc", "train")
 INCLUDE = os.path.join(ROOT, "include")
 HDRS = tuple(os.path.join(INCLUDE, h) for h in ("dropcompute.h", "dropcompute_dev.h", "dropcompute_train.h"))
 LIB = os.path.join(PKG, "libdropcompute.so")
+CALLS = os.path.join(PKG, "_calls.so")
 OBJECTS = os.path.join(PKG, "_build")
 
 COMMON_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
@@ -38,7 +41,7 @@ def _cuda_sources():
 
 
 def _train_sources():
-    return sorted(os.path.join(TRAIN, f) for f in os.listdir(TRAIN) if f.endswith((".cu", ".cuh")))
+    return sorted(os.path.join(TRAIN, f) for f in os.listdir(TRAIN) if f.endswith((".cu", ".cuh", ".cpp")))
 
 
 def source_hash() -> str:
@@ -53,9 +56,9 @@ def source_hash() -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     return any(os.path.getmtime(f) > t for f in (*_cuda_sources(), *_train_sources(), *HDRS, os.path.abspath(__file__)))
 
 
@@ -68,6 +71,27 @@ def _units():
         if f.endswith(".cu"):
             # without unique symbols: a second copy of the library in one process keeps what it knows of its own kernels to itself
             yield f, ["-Xcompiler", "-fno-gnu-unique", "-I", TRAIN], (f, *shared, HDRS[0], HDRS[2])
+
+
+def _compile_calls(force: bool) -> None:
+    """The extension module; it finds the library beside itself and torch's libraries, which are loaded by then."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    lib = os.path.join(root, "lib")
+    src = os.path.join(TRAIN, "calls.cpp")
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(root, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"),
+           "-I", INCLUDE, src, "-L", PKG, "-l:" + os.path.basename(LIB), "-L", lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+           "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib]
+    newest = max(os.path.getmtime(f) for f in (src, HDRS[0], HDRS[2], os.path.abspath(__file__)))
+    if os.path.exists(CALLS) and not force and os.path.getmtime(CALLS) > newest:
+        os.utime(CALLS)
+        return
+    tmp = CALLS + f".tmp{os.getpid()}"
+    res = subprocess.run([*cmd, "-o", tmp], capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"g++ failed on {src}:\n" + res.stdout + res.stderr)
+    os.replace(tmp, CALLS)
 
 
 def _compile(src: str, flags: list, made_from: tuple, force: bool, verbose: bool):
@@ -103,6 +127,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     if res.returncode != 0:
         raise RuntimeError("nvcc failed to link:\n" + res.stdout + res.stderr)
     os.replace(tmp, LIB)
+    _compile_calls(force)
     if verbose:
         print("".join(said for _, said in done))
     return LIB

@@ -1,0 +1,329 @@
+// The training operators' calls with outputs and workspaces from torch's allocator, for api.py: checks, allocation and the call
+// into the C ABI without a step through Python for each of them.  A lookup of 16 tokens costs the host 4 us this way and 8 us
+// through ctypes and torch.empty, a gelu with its three outputs 5 and 12.  Nothing else is here: the work is the C ABI's.
+#include <Python.h>
+
+#include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAGuard.h>
+#include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <string>
+
+#include "dropcompute_train.h"
+
+namespace {
+
+using at::Tensor;
+
+PyObject *g_error = nullptr;   // api.DropComputeError(status, where)
+
+struct Refused { PyObject *type; std::string what; };
+struct Failed { int status; const char *where; };
+struct Raised {};              // a Python error is set already
+
+[[noreturn]] void refuse_type(const std::string &what) { throw Refused{PyExc_TypeError, what}; }
+[[noreturn]] void refuse_value(const std::string &what) { throw Refused{PyExc_ValueError, what}; }
+void done(int status, const char *where)
+{
+    if (status != DC_OK) throw Failed{status, where};
+}
+
+template <class F> PyObject *guarded(F &&f)
+{
+    try {
+        return f();
+    } catch (const Refused &e) {
+        PyErr_SetString(e.type, e.what.c_str());
+    } catch (const Failed &e) {
+        PyObject *x = g_error ? PyObject_CallFunction(g_error, "is", e.status, e.where) : nullptr;
+        if (x) {
+            PyErr_SetObject(reinterpret_cast<PyObject *>(Py_TYPE(x)), x);
+            Py_DECREF(x);
+        } else if (!PyErr_Occurred()) {
+            PyErr_SetString(PyExc_RuntimeError, e.where);
+        }
+    } catch (const Raised &) {
+    } catch (const std::exception &e) {   // torch's own: out of memory and the like
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    }
+    return nullptr;
+}
+
+void arguments(Py_ssize_t got, Py_ssize_t want)
+{
+    if (got != want) refuse_type("takes " + std::to_string(want) + " arguments, got " + std::to_string(got));
+}
+const Tensor &tensor(PyObject *o, const char *name)
+{
+    if (!THPVariable_Check(o)) refuse_type(std::string(name) + " must be a CUDA tensor");
+    const Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda()) refuse_type(std::string(name) + " must be a CUDA tensor");
+    return t;
+}
+int64_t whole(PyObject *o)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Raised{};
+    return v;
+}
+float real(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Raised{};
+    return static_cast<float>(v);
+}
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised{};
+    return v != 0;
+}
+std::string shown(at::IntArrayRef s)
+{
+    std::string r = "(";
+    for (size_t i = 0; i < s.size(); ++i) r += (i ? ", " : "") + std::to_string(s[i]);
+    return r + ")";
+}
+
+int32_t code(at::ScalarType t)
+{
+    return t == at::kBFloat16 ? DC_BF16 : t == at::kHalf ? DC_F16 : t == at::kFloat ? DC_F32 : -1;
+}
+
+struct Matrix { void *p; int64_t stride, rows, cols; int32_t dtype; };
+
+// A tensor as a matrix: adjacent elements in a row, evenly spaced rows, leading dimensions flattened.
+Matrix matrix(const Tensor &t, const char *name, const Tensor *beside = nullptr, bool same_type = false)
+{
+    const int32_t c = code(t.scalar_type());
+    if (c < 0 || (same_type && t.scalar_type() != beside->scalar_type()))
+        refuse_type(std::string(name) + " must be " + (same_type ? c10::toString(beside->scalar_type()) : "bfloat16, float16 or float32") + ", got " +
+                    c10::toString(t.scalar_type()));
+    if (beside && t.device() != beside->device()) refuse_value(std::string(name) + " is on " + t.device().str() + ", not " + beside->device().str());
+    const int64_t dims = t.dim();
+    if (dims < 1) refuse_value(std::string(name) + " must have at least one dimension");
+    const auto sizes = t.sizes(), strides = t.strides();
+    const int64_t cols = sizes[dims - 1];
+    int64_t rows = 1;
+    for (int64_t i = 0; i + 1 < dims; ++i) rows *= sizes[i];
+    if (cols > 1 && rows > 0 && strides[dims - 1] != 1) refuse_value("the elements of a row of " + std::string(name) + " must be adjacent");
+    // the innermost leading dimension that is more than one row sets the distance, the others have to continue it
+    int64_t stride = 0, span = 1;
+    for (int64_t i = dims - 2; i >= 0 && rows > 1; --i) {
+        if (sizes[i] == 1) continue;
+        if (stride == 0) stride = strides[i];
+        else if (strides[i] != stride * span) refuse_value("the rows of " + std::string(name) + " must be evenly spaced");
+        span *= sizes[i];
+    }
+    return {t.data_ptr(), rows > 1 ? stride : std::max<int64_t>(1, cols), rows, cols, c};
+}
+
+void *vector(const Tensor &t, const char *name, at::ScalarType type, int64_t n, const Tensor &beside)
+{
+    if (t.scalar_type() != type) refuse_type(std::string(name) + " must be " + c10::toString(type) + ", got " + c10::toString(t.scalar_type()));
+    if (t.device() != beside.device()) refuse_value(std::string(name) + " is on " + t.device().str() + ", not " + beside.device().str());
+    if (!t.is_contiguous()) refuse_value(std::string(name) + " must be contiguous");
+    if (t.numel() != n) refuse_value(std::string(name) + " must hold " + std::to_string(n) + " values, got " + std::to_string(t.numel()));
+    return t.data_ptr();
+}
+
+Tensor make(at::IntArrayRef sizes, at::ScalarType type, const Tensor &beside) { return at::empty(sizes, beside.options().dtype(type).requires_grad(false)); }
+Tensor workspace(PyObject *given, size_t bytes, const Tensor &beside)
+{
+    if (given == Py_None) return make({static_cast<int64_t>(bytes)}, at::kByte, beside);
+    const Tensor &t = tensor(given, "workspace");
+    vector(t, "workspace", at::kByte, t.numel(), beside);
+    return t;
+}
+void *stream(const Tensor &t) { return c10::cuda::getCurrentCUDAStream(t.get_device()).stream(); }
+PyObject *wrap(const Tensor &t) { return THPVariable_Wrap(t); }
+PyObject *two(PyObject *a, PyObject *b)
+{
+    PyObject *r = PyTuple_New(2);
+    PyTuple_SET_ITEM(r, 0, a);
+    PyTuple_SET_ITEM(r, 1, b);
+    return r;
+}
+PyObject *none()
+{
+    Py_INCREF(Py_None);
+    return Py_None;
+}
+
+// embed(table, ids, scale, pad_id)
+PyObject *embed(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        arguments(n, 4);
+        const Tensor &table = tensor(a[0], "table"), &ids = tensor(a[1], "ids");
+        const Matrix t = matrix(table, "table");
+        const int64_t N = ids.numel();
+        const auto *i = static_cast<const int64_t *>(vector(ids, "ids", at::kLong, N, table));
+        const c10::cuda::CUDAGuard on(table.device());
+        at::DimVector shape(ids.sizes().begin(), ids.sizes().end());
+        shape.push_back(t.cols);
+        const Tensor out = make(shape, table.scalar_type(), table);
+        done(dc_embed(t.p, t.stride, t.dtype, i, N, t.rows, t.cols, real(a[2]), whole(a[3]), out.data_ptr(), t.cols, stream(table)), "dc_embed");
+        return wrap(out);
+    });
+}
+
+// embed_backward(dout, ids, V, scale, pad_id, dtable or None, accumulate, the dtype of a new dtable (a tensor's code) or -1, workspace or None)
+PyObject *embed_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        arguments(n, 9);
+        const Tensor &dout = tensor(a[0], "dout"), &ids = tensor(a[1], "ids");
+        const Matrix d = matrix(dout, "dout");
+        const auto *i = static_cast<const int64_t *>(vector(ids, "ids", at::kLong, d.rows, dout));
+        const int64_t V = whole(a[2]), as = whole(a[7]);
+        const bool accumulate = truth(a[6]);
+        const c10::cuda::CUDAGuard on(dout.device());
+        Tensor table;
+        if (a[5] == Py_None) {
+            if (accumulate) refuse_value("accumulate needs the dtable to add to");
+            const at::ScalarType type = as < 0 ? dout.scalar_type() : as == DC_BF16 ? at::kBFloat16 : as == DC_F16 ? at::kHalf : at::kFloat;
+            if (V < 1) refuse_value("V must be positive");
+            table = make({V, d.cols}, type, dout);
+        } else {
+            table = tensor(a[5], "dtable");
+        }
+        const Matrix t = matrix(table, "dtable", &dout);
+        if (table.dim() != 2 || t.rows != V || t.cols != d.cols)
+            refuse_value("dtable must be (" + std::to_string(V) + ", " + std::to_string(d.cols) + "), got " + shown(table.sizes()));
+        const Tensor ws = workspace(a[8], dc_embed_backward_workspace_bytes(d.rows, V, d.cols), dout);
+        done(dc_embed_backward(d.p, d.stride, d.dtype, i, d.rows, V, d.cols, real(a[3]), whole(a[4]), t.p, t.stride, t.dtype, accumulate, ws.data_ptr(),
+                               static_cast<size_t>(ws.numel()), stream(dout)), "dc_embed_backward");
+        return wrap(table);
+    });
+}
+
+// gelu_save8(x) -> (y, q, scales)
+PyObject *gelu_save8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        arguments(n, 1);
+        const Tensor &x = tensor(a[0], "x");
+        const Matrix m = matrix(x, "x");
+        const c10::cuda::CUDAGuard on(x.device());
+        at::DimVector groups(x.sizes().begin(), x.sizes().end());
+        groups.back() = (m.cols + DC_SAVE8_GROUP - 1) / DC_SAVE8_GROUP;
+        const Tensor y = make(x.sizes(), x.scalar_type(), x), q = make(x.sizes(), at::kChar, x), scales = make(groups, at::kFloat, x);
+        done(dc_gelu_save8(m.p, m.stride, m.dtype, m.rows, m.cols, y.data_ptr(), m.cols, static_cast<int8_t *>(q.data_ptr()), static_cast<float *>(scales.data_ptr()),
+                           stream(x)), "dc_gelu_save8");
+        PyObject *r = PyTuple_New(3);
+        PyTuple_SET_ITEM(r, 0, wrap(y));
+        PyTuple_SET_ITEM(r, 1, wrap(q));
+        PyTuple_SET_ITEM(r, 2, wrap(scales));
+        return r;
+    });
+}
+
+// gelu_save8_backward(dy, q, scales, want_y) -> dx, or (dx, y)
+PyObject *gelu_save8_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        arguments(n, 4);
+        const Tensor &dy = tensor(a[0], "dy"), &q = tensor(a[1], "q"), &scales = tensor(a[2], "scales");
+        const Matrix d = matrix(dy, "dy");
+        const auto *qp = static_cast<const int8_t *>(vector(q, "q", at::kChar, d.rows * d.cols, dy));
+        const auto *sp = static_cast<const float *>(vector(scales, "scales", at::kFloat, d.rows * ((d.cols + DC_SAVE8_GROUP - 1) / DC_SAVE8_GROUP), dy));
+        const bool want_y = truth(a[3]);
+        const c10::cuda::CUDAGuard on(dy.device());
+        const Tensor dx = make(dy.sizes(), dy.scalar_type(), dy);
+        Tensor y;
+        if (want_y) y = make(dy.sizes(), dy.scalar_type(), dy);
+        done(dc_gelu_save8_backward(d.p, d.stride, d.dtype, qp, sp, d.rows, d.cols, dx.data_ptr(), d.cols, want_y ? y.data_ptr() : nullptr, d.cols, stream(dy)),
+             "dc_gelu_save8_backward");
+        return want_y ? two(wrap(dx), wrap(y)) : wrap(dx);
+    });
+}
+
+struct Loss { Matrix h, w; const int64_t *targets; };
+Loss loss_inputs(const Tensor &hidden, const Tensor &weight, const Tensor &targets)
+{
+    Loss l;
+    l.h = matrix(hidden, "hidden");
+    l.w = matrix(weight, "weight", &hidden, true);
+    if (l.w.cols != l.h.cols) refuse_value("weight must be (" + std::to_string(l.w.rows) + ", " + std::to_string(l.h.cols) + "), got " + shown(weight.sizes()));
+    l.targets = static_cast<const int64_t *>(vector(targets, "targets", at::kLong, l.h.rows, hidden));
+    return l;
+}
+
+// vocab_loss(hidden, weight, targets, ignore_index, logit_scale, workspace or None) -> (loss, lse)
+PyObject *vocab_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        arguments(n, 6);
+        const Tensor &hidden = tensor(a[0], "hidden"), &weight = tensor(a[1], "weight"), &targets = tensor(a[2], "targets");
+        const Loss l = loss_inputs(hidden, weight, targets);
+        const c10::cuda::CUDAGuard on(hidden.device());
+        const Tensor loss = make(targets.sizes(), at::kFloat, hidden), lse = make(targets.sizes(), at::kFloat, hidden);
+        const Tensor ws = workspace(a[5], dc_vocab_loss_workspace_bytes(l.h.rows, l.w.rows, l.h.cols, l.w.p, l.w.stride, 0), hidden);
+        done(dc_vocab_loss(l.h.p, l.h.stride, l.w.p, l.w.stride, l.h.dtype, l.targets, l.h.rows, l.w.rows, l.h.cols, whole(a[3]), real(a[4]),
+                           static_cast<float *>(loss.data_ptr()), static_cast<float *>(lse.data_ptr()), ws.data_ptr(), static_cast<size_t>(ws.numel()), stream(hidden)),
+             "dc_vocab_loss");
+        return two(wrap(loss), wrap(lse));
+    });
+}
+
+// vocab_loss_backward(hidden, weight, targets, lse, dloss, ignore_index, logit_scale, dweight or None, accumulate, want_dhidden, want_dweight,
+// workspace or None) -> (dhidden or None, dweight or None)
+PyObject *vocab_loss_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        arguments(n, 12);
+        const Tensor &hidden = tensor(a[0], "hidden"), &weight = tensor(a[1], "weight"), &targets = tensor(a[2], "targets");
+        const Loss l = loss_inputs(hidden, weight, targets);
+        const auto *lse = static_cast<const float *>(vector(tensor(a[3], "lse"), "lse", at::kFloat, l.h.rows, hidden));
+        const auto *dloss = static_cast<const float *>(vector(tensor(a[4], "dloss"), "dloss", at::kFloat, l.h.rows, hidden));
+        const bool accumulate = truth(a[8]), want_dh = truth(a[9]), want_dw = truth(a[10]);
+        if (accumulate && a[7] == Py_None) refuse_value("accumulate needs the dweight to add to");
+        const c10::cuda::CUDAGuard on(hidden.device());
+        Tensor dh, dw;
+        if (want_dh) dh = make(hidden.sizes(), hidden.scalar_type(), hidden);
+        Matrix d{nullptr, 0, 0, 0, l.h.dtype};
+        if (a[7] != Py_None) dw = tensor(a[7], "dweight");
+        else if (want_dw) dw = make(weight.sizes(), weight.scalar_type(), weight);
+        if (dw.defined()) {
+            d = matrix(dw, "dweight", &hidden);
+            if (d.rows != l.w.rows || d.cols != l.w.cols)
+                refuse_value("dweight must be (" + std::to_string(l.w.rows) + ", " + std::to_string(l.w.cols) + "), got " + shown(dw.sizes()));
+        }
+        const Tensor ws = workspace(a[11], dc_vocab_loss_workspace_bytes(l.h.rows, l.w.rows, l.h.cols, l.w.p, l.w.stride, 1), hidden);
+        done(dc_vocab_loss_backward(l.h.p, l.h.stride, l.w.p, l.w.stride, l.h.dtype, l.targets, l.h.rows, l.w.rows, l.h.cols, whole(a[5]), real(a[6]), lse, dloss,
+                                    want_dh ? dh.data_ptr() : nullptr, l.h.cols, d.p, d.stride, d.dtype, accumulate, ws.data_ptr(),
+                                    static_cast<size_t>(ws.numel()), stream(hidden)), "dc_vocab_loss_backward");
+        return two(want_dh ? wrap(dh) : none(), dw.defined() ? wrap(dw) : none());
+    });
+}
+
+// raise_with(class): what a status that is not DC_OK is raised as
+PyObject *raise_with(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&] {
+        arguments(n, 1);
+        Py_INCREF(a[0]);
+        Py_XDECREF(g_error);
+        g_error = a[0];
+        return none();
+    });
+}
+
+PyCFunction fast(PyObject *(*f)(PyObject *, PyObject *const *, Py_ssize_t)) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(f)); }
+PyMethodDef methods[] = {
+    {"embed", fast(embed), METH_FASTCALL, nullptr},
+    {"embed_backward", fast(embed_backward), METH_FASTCALL, nullptr},
+    {"gelu_save8", fast(gelu_save8), METH_FASTCALL, nullptr},
+    {"gelu_save8_backward", fast(gelu_save8_backward), METH_FASTCALL, nullptr},
+    {"vocab_loss", fast(vocab_loss), METH_FASTCALL, nullptr},
+    {"vocab_loss_backward", fast(vocab_loss_backward), METH_FASTCALL, nullptr},
+    {"raise_with", fast(raise_with), METH_FASTCALL, nullptr},
+    {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__calls() { return PyModule_Create(&module_def); }
