@@ -31,13 +31,15 @@ struct Gather {
     int64_t N, V; int32_t D, Dp;
     int32_t per_block;                     // rows of a block, a multiple of 32
     float logit_scale;
-    const void *weight; int64_t ws;        // rows start on 16-byte boundaries
+    const void *weight; int64_t ws;
+    void *copy; int32_t blocks;            // a copy of the weight [V][Dp], where its own rows do not start on 16-byte boundaries; blocks that gather
     Head *head; int32_t *row_of, *pos_of, *label; float *row_hit, *row_lse, *row_factor;
     void *rows;                            // [Lp][Dp]
     float *loss_out, *lse_out;             // forward only: rows without a label are written here
     int32_t vocab_blocks, pairs; int64_t acc_rows;
 };
 
+// Blocks from a.blocks on make the copy of the weight that bulk tensor copies can read, where one is needed.
 // Every block counts the labelled rows before its own, and in the backward pass finds the largest factor |dloss c|, by itself:
 // a few bytes per row from L2, and no block waits for another.
 template <class T, int V>
@@ -49,8 +51,16 @@ __global__ void __launch_bounds__(kGatherThreads) vocab_gather(const __grid_cons
     __shared__ int32_t where[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t first = (int64_t)blockIdx.x * a.per_block, end = min(a.N, first + a.per_block);
-    const bool last_block = blockIdx.x == gridDim.x - 1;
+    const bool last_block = (int32_t)blockIdx.x == a.blocks - 1;
     follow();
+    if ((int32_t)blockIdx.x >= a.blocks) {
+        const T *w = (const T *)a.weight;
+        T *to = (T *)a.copy;
+        for (int64_t v = (int64_t)(blockIdx.x - a.blocks) * W + warp; v < a.V; v += (int64_t)(gridDim.x - a.blocks) * W)
+#pragma unroll 4
+            for (int32_t d = lane; d < a.Dp; d += 32) to[v * a.Dp + d] = d < a.D ? w[v * a.ws + d] : from_f<T>(0.0f);
+        return;
+    }
     int32_t c = 0;
     float m = 0.0f;
     const int64_t look = a.dloss ? a.N : first;
@@ -147,15 +157,6 @@ __global__ void __launch_bounds__(kGatherThreads) vocab_gather(const __grid_cons
         const int64_t from = (int64_t)base * a.Dp, to = ceil_div(base, kRowBlock) * kRowBlock * (int64_t)a.Dp;
         for (int64_t d = from + tid * 8; d < to; d += kGatherThreads * 8) *reinterpret_cast<uint4 *>(rows + d) = make_uint4(0, 0, 0, 0);
     }
-}
-
-// A copy of the weight with rows that start on 16-byte boundaries, where its own do not.
-template <class T>
-__global__ void __launch_bounds__(256) vocab_copy_weight(const T *__restrict__ w, int64_t ws, int64_t V, int32_t D, int32_t Dp, T *__restrict__ to)
-{
-    follow();
-    for (int64_t v = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); v < V; v += (int64_t)gridDim.x * 8)
-        for (int32_t d = threadIdx.x & 31; d < Dp; d += 32) to[v * Dp + d] = d < D ? w[v * ws + d] : from_f<T>(0.0f);
 }
 
 // ---- joining the tiles of the vocabulary: a warp per row --------------------------------------------------------------------
@@ -278,25 +279,18 @@ inline int check(const void *hidden, int64_t hs, const void *weight, int64_t ws,
     return DC_OK;
 }
 
+// Gathers the rows, and leaves in weight and ws one that bulk tensor copies can read.
 template <class T>
-int gather(Gather &g, const Plan &p, const void *weight, int64_t ws, cudaStream_t st)
+int gather(Gather &g, const Plan &p, const void **weight, int64_t *ws, cudaStream_t st)
 {
-    g.weight = weight; g.ws = ws; g.row_hit = p.row_hit;
+    g.weight = *weight; g.ws = *ws; g.row_hit = p.row_hit; g.copy = p.copy_weight ? p.weight : nullptr;
     g.per_block = (int32_t)(ceil_div(ceil_div(g.N, kGatherBlocks), 32) * 32);
-    const unsigned blocks = (unsigned)ceil_div(g.N, g.per_block);
-    const bool wide = g.D % 8 == 0 && rows_on(g.hidden, g.hs, 2, 16);
-    return launch(wide ? vocab_gather<T, 8> : vocab_gather<T, 1>, dim3(blocks), kGatherThreads, 0, st, g);
-}
-
-// The weight as bulk tensor copies can read it.
-template <class T>
-int readable(const Plan &p, const Gather &g, const void **weight, int64_t *ws, cudaStream_t st)
-{
-    if (!p.copy_weight) return DC_OK;
-    const int e = launch(vocab_copy_weight<T>, dim3((unsigned)(sm_count() * 8)), 256, 0, st, (const T *)*weight, *ws, g.V, g.D, p.Dp, (T *)p.weight);
-    *weight = p.weight;
-    *ws = p.Dp;
-    return e;
+    g.blocks = (int32_t)ceil_div(g.N, g.per_block);
+    const int64_t rows_to_copy = ceil_div(g.V, kGatherThreads / 32), most = (int64_t)sm_count() * 4;
+    const int64_t copying = !p.copy_weight ? 0 : rows_to_copy < most ? rows_to_copy : most;
+    if (p.copy_weight) { *weight = p.weight; *ws = p.Dp; }
+    const bool wide = g.D % 8 == 0 && rows_on(g.hidden, g.hs, 2, 16) && !p.copy_weight;
+    return launch(wide ? vocab_gather<T, 8> : vocab_gather<T, 1>, dim3((unsigned)(g.blocks + copying)), kGatherThreads, 0, st, g);
 }
 
 template <class T>
@@ -321,8 +315,7 @@ int forward(Gather g, const Plan &p, const void *weight, int64_t ws, float *loss
     Product q{};
     if (!tensor_map(&a, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&b, p.copy_weight ? p.weight : weight, bf, g.D, g.V, p.copy_weight ? p.Dp : ws, 128))
         return DC_ERR_CUDA;
-    if (int e = readable<T>(p, g, &weight, &ws, st)) return e;
-    if (int e = gather<T>(g, p, weight, ws, st)) return e;
+    if (int e = gather<T>(g, p, &weight, &ws, st)) return e;
     q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.part = p.part; q.hit = p.hit; q.part_pitch = 2 * p.tiles_v;
     q.V = (int32_t)g.V; q.D = g.D; q.Dp = p.Dp;
     if (int e = launch_units<T, kLoss>(p.Lp / kTileM * p.tiles_v, pairs, a, b, a, b, q, st)) return e;
@@ -336,8 +329,7 @@ int backward(Gather g, const Plan &p, const void *weight, int64_t ws, void *dh, 
     const int32_t pairs = pairs_on_device<T>();
     if (pairs == 0) return DC_ERR_CUDA;
     g.vocab_blocks = p.vocab_blocks; g.pairs = pairs; g.acc_rows = p.acc_rows;
-    if (int e = readable<T>(p, g, &weight, &ws, st)) return e;
-    if (int e = gather<T>(g, p, weight, ws, st)) return e;
+    if (int e = gather<T>(g, p, &weight, &ws, st)) return e;
     const int ob = dw_f32 ? 4 : 2;
     CUtensorMap rows, rows_mn, grad_k, grad_mn;
     if (!tensor_map(&rows, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&grad_k, p.grad, bf, p.piece, p.Lp, p.piece, 128) ||
