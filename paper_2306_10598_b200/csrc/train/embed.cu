@@ -13,6 +13,7 @@ constexpr int kSumThreads = 64;
 constexpr int kBuckets = 128;        // blocks of embed_sort; more where a bucket would hold more than kMaxKeys tokens
 constexpr int kMaxKeys = 4096;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+static_assert(kSortWarps == 32, "a lane has the counts of a warp");
 constexpr int kWarpList = 128, kList = kSortWarps * kWarpList;   // places of a bucket that are put in order at a time
 
 // ---- lookup: a warp takes (row, chunk of columns), packs_of(V) packs to a lane ------------------------------------------------

@@ -5,15 +5,18 @@
 // 128 is held by 128/V lanes with V adjacent elements each (V = 16 bytes' worth), which makes its maximum a few shuffles and
 // leaves nothing to pass through shared memory.  Conversions between integers and floats, which would go to the
 // special-function unit too, are done by adding a constant whose last bits are the integer.
+#include <type_traits>
+
 #include "train_common.cuh"
 
 namespace dct {
 
 constexpr int kGroup = DC_SAVE8_GROUP;
 // Blocks of 128 threads; a thread has two groups on their way in the forward pass and one in the backward pass.  16384 x 8192
-// bf16, us forward / backward: 128 threads 124 / 152 (one group), 117 / 162 (two), 118 / 162 (four); 256 threads 126 / 152, 120 /
-// 166, 127 / 175; 512 threads 128 / 156 (one).  Memory takes 3.7 TB/s when it is only written (fill of 268 MB: 72 us), so the
-// bytes written alone need 109 / 145.
+// bf16, us: forward 138 with one group, 123 with two, 124 with four; forward / backward 139 / 271 in blocks of 64, 130 / 145 of 256
+// threads, 123 / 143 of 128.  Memory takes 3.7 TB/s when it is only written (fill of 268 MB: 72 us), so the bytes written alone
+// need 109 / 145; 5.4 and 6.6 TB/s of all bytes.  Rows off 16 bytes, an element to a load: 16384 x 4095 109 / 137, bound by the
+// instructions issued.
 constexpr int kThreads = 128;
 constexpr int kAheadForward = 2, kAheadBackward = 1;
 constexpr float kTwoA = 1.5957691216057308f;                   // 2 sqrt(2/pi)
@@ -89,10 +92,13 @@ template <class T, int V, int kAhead> struct Hold {
     static constexpr int GAP = kThreads / LPG, PER = GAP * kAhead;
 };
 
-// Where the groups of a thread are, as (row, first column).  FLAT: the matrix is one row of whole groups.
+// Where the groups of a thread are, as (row, first column).  FLAT: the matrix is one row of whole groups.  Columns of a row are
+// counted in 32 bits otherwise: rows that start anywhere leave an element to a load, and its address is most of the work.
+template <bool FLAT> using Column = std::conditional_t<FLAT, int64_t, int32_t>;
 template <bool FLAT> struct Groups {
-    int64_t row, col, drow, dcol, D, wrap;
-    __device__ Groups(int64_t first, int64_t gap, int64_t per_row, int64_t D_) : D(D_)
+    int64_t row, drow;
+    Column<FLAT> col, dcol, D, wrap;
+    __device__ Groups(int64_t first, int32_t gap, int64_t per_row, int64_t D_) : D((Column<FLAT>)D_)
     {
         if (FLAT) {
             row = 0;
@@ -100,12 +106,12 @@ template <bool FLAT> struct Groups {
             dcol = gap * kGroup;
             return;
         }
-        // the only divisions of a thread, in 32 bits where they can be: they are a good part of its work otherwise
+        // the only divisions of a thread, in 32 bits where they can be
         row = (first | per_row) >> 32 ? first / per_row : (int64_t)((uint32_t)first / (uint32_t)per_row);
-        col = (first - row * per_row) * kGroup;
+        col = (Column<FLAT>)((first - row * per_row) * kGroup);
         drow = gap < per_row ? 0 : (uint32_t)gap / (uint32_t)per_row;
-        dcol = (gap - drow * per_row) * kGroup;
-        wrap = per_row * kGroup;
+        dcol = (Column<FLAT>)((gap - drow * per_row) * kGroup);
+        wrap = (Column<FLAT>)(per_row * kGroup);
     }
     __device__ __forceinline__ void next()
     {
@@ -127,26 +133,33 @@ __global__ void __launch_bounds__(kThreads) gelu_save8_kernel(const T *__restric
     Groups<FLAT> g(first, H::GAP, per_row, D);
     follow();
     Pack<T, V> p[kAhead][H::K];
-    int64_t row[kAhead], col[kAhead];
+    int64_t row[kAhead];
+    Column<FLAT> col[kAhead], left[kAhead];                    // first column of this thread's packs, and columns from there to the end
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
         row[u] = g.row;
-        col[u] = g.col;
+        col[u] = g.col + lane * V;
+        left[u] = g.row < N ? g.D - col[u] : 0;
+        const T *from = x + row[u] * xs + col[u];
 #pragma unroll
         for (int k = 0; k < H::K; ++k) {
-            const int64_t c = col[u] + (k * H::LPG + lane) * V;
             p[u][k] = Pack<T, V>{};
-            if (row[u] < N && c < D) p[u][k] = *reinterpret_cast<const Pack<T, V> *>(x + row[u] * xs + c);
+            if (left[u] > k * H::LPG * V) p[u][k] = *reinterpret_cast<const Pack<T, V> *>(from + k * H::LPG * V);
         }
         g.next();
     }
     Top<T> top[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
+        if constexpr (V > 1) {
 #pragma unroll
-        for (int k = 0; k < H::K; ++k)
+            for (int k = 0; k < H::K; ++k)
 #pragma unroll
-            for (int i = 0; i < V; i += 2) top[u].add(p[u][k].v[i], p[u][k].v[V > 1 ? i + 1 : i]);
+                for (int i = 0; i < V; i += 2) top[u].add(p[u][k].v[i], p[u][k].v[i + 1]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < H::K; k += 2) top[u].add(p[u][k].v[0], p[u][k + 1].v[0]);
+        }
 #pragma unroll
         for (int d = H::LPG / 2; d; d >>= 1) top[u].swap(d);
     }
@@ -155,13 +168,12 @@ __global__ void __launch_bounds__(kThreads) gelu_save8_kernel(const T *__restric
         const float a = top[u].value();
         const bool finite = a < INFINITY, live = a > 0x1p-100f && finite;
         const float inv = live ? __fdiv_rn(127.0f, a) : 0.0f;
-        if (row[u] >= N) continue;
-        if (lane == 0) scales[row[u] * per_row + col[u] / kGroup] = live ? __fmul_rn(a, 1.0f / 127.0f) : finite ? 0.0f : __uint_as_float(0x7fffffffu);
+        if (lane == 0 && row[u] < N) scales[row[u] * per_row + col[u] / kGroup] = live ? __fmul_rn(a, 1.0f / 127.0f) : finite ? 0.0f : __uint_as_float(0x7fffffffu);
+        T *to = y + row[u] * ys + col[u];
+        int8_t *bytes = q + row[u] * D + col[u];
 #pragma unroll
         for (int k = 0; k < H::K; ++k) {
-            const int64_t c = col[u] + (k * H::LPG + lane) * V;
-            if (c >= D) continue;
-            Pack<T, V> o;
+            Pack<T, V> o;                                      // worked out whether it is stored or not, so that packs overlap
             uint32_t n[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -169,8 +181,10 @@ __global__ void __launch_bounds__(kThreads) gelu_save8_kernel(const T *__restric
                 o.v[i] = from_f<T>(v * gate(v));
                 n[i] = nearest(live ? __fmul_rn(v, inv) : 0.0f);
             }
-            *reinterpret_cast<Pack<T, V> *>(y + row[u] * ys + c) = o;
-            *reinterpret_cast<Bytes<V> *>(q + row[u] * D + c) = bytes_of<V>(n);
+            if (left[u] > k * H::LPG * V) {
+                *reinterpret_cast<Pack<T, V> *>(to + k * H::LPG * V) = o;
+                *reinterpret_cast<Bytes<V> *>(bytes + k * H::LPG * V) = bytes_of<V>(n);
+            }
         }
     }
 }
@@ -186,43 +200,38 @@ __global__ void __launch_bounds__(kThreads) gelu_save8_backward_kernel(const T *
     const int64_t per_row = (D + kGroup - 1) / kGroup, first = (int64_t)blockIdx.x * H::PER + threadIdx.x / H::LPG;
     Groups<FLAT> g(first, H::GAP, per_row, D);
     follow();
-    Pack<T, V> p[kAhead][H::K];
-    Bytes<V> b[kAhead][H::K];
-    float scale[kAhead];
-    int64_t row[kAhead], col[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-        row[u] = g.row;
-        col[u] = g.col;
-        if (row[u] < N) scale[u] = scales[row[u] * per_row + col[u] / kGroup];
+        const Column<FLAT> col = g.col + lane * V, left = g.row < N ? g.D - col : 0;
+        if (left <= 0) { g.next(); continue; }
+        Pack<T, V> p[H::K];
+        Bytes<V> b[H::K];
+        const float scale = scales[g.row * per_row + col / kGroup];
+        const T *from = dy + g.row * dys + col;
+        const int8_t *bytes = q + g.row * D + col;
 #pragma unroll
-        for (int k = 0; k < H::K; ++k) {
-            const int64_t c = col[u] + (k * H::LPG + lane) * V;
-            if (row[u] < N && c < D) {
-                p[u][k] = *reinterpret_cast<const Pack<T, V> *>(dy + row[u] * dys + c);
-                b[u][k] = *reinterpret_cast<const Bytes<V> *>(q + row[u] * D + c);
+        for (int k = 0; k < H::K; ++k)
+            if (left > k * H::LPG * V) {
+                p[k] = *reinterpret_cast<const Pack<T, V> *>(from + k * H::LPG * V);
+                b[k] = *reinterpret_cast<const Bytes<V> *>(bytes + k * H::LPG * V);
             }
-        }
-        g.next();
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+        T *to = dx + g.row * dxs + col, *again = y + g.row * ys + col;
 #pragma unroll
         for (int k = 0; k < H::K; ++k) {
-            const int64_t c = col[u] + (k * H::LPG + lane) * V;
-            if (row[u] >= N || c >= D) continue;
+            if (left <= k * H::LPG * V) break;
             Pack<T, V> o, r;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float v = whole(b[u][k], i) * scale[u], s = gate(v);
+                const float v = whole(b[k], i) * scale, s = gate(v);
                 const float near = fminf(fmaxf(v, -64.0f), 64.0f);   // beyond, s (1 - s) is 0 and v^2 must not make it NaN
                 const float slope = fmaf(near * fmaf(3.0f * kB * kTwoA, near * near, kTwoA), fmaf(-s, s, s), s);   // NaN where v is: s is
-                o.v[i] = from_f<T>(to_f(p[u][k].v[i]) * slope);
+                o.v[i] = from_f<T>(to_f(p[k].v[i]) * slope);
                 r.v[i] = from_f<T>(v * s);
             }
-            *reinterpret_cast<Pack<T, V> *>(dx + row[u] * dxs + c) = o;
-            if (y) *reinterpret_cast<Pack<T, V> *>(y + row[u] * ys + c) = r;
+            *reinterpret_cast<Pack<T, V> *>(to + k * H::LPG * V) = o;
+            if (y) *reinterpret_cast<Pack<T, V> *>(again + k * H::LPG * V) = r;
         }
+        g.next();
     }
 }
 
