@@ -3,7 +3,7 @@
 // The gradient of a token is the sum over every place where it occurs; tokens of text fall like 1 / rank, so one token
 // can hold several per cent of all places.  Places are grouped by token first (embed_sort), and the sum then runs over
 // equal tiles of the grouped list, whatever the tokens are: a token that is spread over several tiles leaves one partial
-// sum per tile, which embed_join adds in order.  No floating-point atomics, so two calls give the same bits.
+// sum per tile, which embed_join adds in order.  No element is added to twice in a call, so two calls give the same bits.
 #include "train_common.cuh"
 
 namespace dct {
@@ -33,10 +33,11 @@ __global__ void __launch_bounds__(256) embed_kernel(const T *__restrict__ table,
     const int64_t c0 = (task - n * chunks) * (U * 32 * V) + lane * V;
     const int64_t id = ids[n];
     T *o = out + n * os;
-    if (id == pad || id < 0 || id >= vocab) {
+    const bool is_pad = pad >= 0 && id == pad;
+    if (is_pad || id < 0 || id >= vocab) {
         Pack<T, V> fill;
 #pragma unroll
-        for (int i = 0; i < V; ++i) fill.v[i] = from_f<T>(id == pad ? 0.0f : __uint_as_float(0x7fffffffu));
+        for (int i = 0; i < V; ++i) fill.v[i] = from_f<T>(is_pad ? 0.0f : __uint_as_float(0x7fffffffu));
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (c0 + u * 32 * V < D) *reinterpret_cast<Pack<T, V> *>(o + c0 + u * 32 * V) = fill;
@@ -60,7 +61,9 @@ __global__ void __launch_bounds__(256) embed_kernel(const T *__restrict__ table,
 
 // Block b collects the places of tokens with token mod buckets = b, in order of place, and writes them token by token.
 // Every block reads all ids (from L2, eight loads of a thread in flight), so it also counts what goes before its own part and
-// no block waits for another.  16384 ids of 32768 tokens: see the figures at embed_sum.
+// no block waits for another.  16384 ids take 9 us, 65536 24 us, bound by the instructions that look at an id (68 % of the issue
+// slots) and at small sizes by the few steps that follow one another.  A token that holds more than a sixteenth of 65536 places
+// overflows its warps' lists, and they are collected again: 65 us.
 __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__restrict__ ids, int32_t N, int64_t vocab, int64_t pad, int32_t log_buckets,
                                                            int32_t *__restrict__ place, int32_t *__restrict__ token, int32_t *__restrict__ live,
                                                            uint8_t *__restrict__ occurs)
@@ -492,7 +495,6 @@ extern "C" int dc_embed(const void *table, int64_t table_stride, int32_t dtype, 
     if (table_stride < D || out_stride < D) return DC_ERR_SHAPE;
     const int eb = elem_bytes(dtype);
     if (!on(table, eb) || !on(out, eb) || !on(ids, 8)) return DC_ERR_ALIGN;
-    if (pad_id < 0) pad_id = INT64_MIN;
     const bool wide = D % (16 / eb) == 0 && rows_on(table, table_stride, eb, 16) && rows_on(out, out_stride, eb, 16);
     const cudaStream_t st = (cudaStream_t)stream;
 #define DCT_LOOKUP(T, W) lookup<T, W>(table, table_stride, ids, N, V, D, scale, pad_id, out, out_stride, st)
@@ -528,7 +530,6 @@ extern "C" int dc_embed_backward(const void *dout, int64_t dout_stride, int32_t 
     if (sm_count() == 0) return DC_ERR_CUDA;
     const Work w = carve(workspace, N, V, D);
     const SortPlan p = sort_plan(V);
-    if (pad_id < 0) pad_id = INT64_MIN;
     if (int e = launch(embed_sort, dim3(1u << p.log_buckets), kSortThreads, (size_t)p.keys * 4, st, ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token,
                        w.live, accumulate ? nullptr : w.occurs)) return e;
     // packs of 16 bytes of dout, and of as many elements of dtable

@@ -141,9 +141,10 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
-// log sum exp with the label's logit `hit`, as the tensor cores formed it, replaced by `exact`
+// log sum exp with the label's logit `hit`, as the tensor cores formed it, replaced by `exact`; as it is where one is not finite
 __device__ __forceinline__ float with_label(float lse, float hit, float exact)
 {
+    if (!(fabsf(exact - hit) < INFINITY)) return lse;
     return lse + log1pf(__expf(hit - lse) * expm1f(exact - hit));
 }
 

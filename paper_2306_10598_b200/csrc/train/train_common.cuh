@@ -50,7 +50,9 @@ template <class... P, class... A> int launch(void (*kernel)(P...), dim3 grid, in
     at[0].val.programmaticStreamSerializationAllowed = 1;
     c.attrs = at;
     c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...) == cudaSuccess ? DC_OK : DC_ERR_CUDA;
+    if (cudaLaunchKernelEx(&c, kernel, static_cast<P>(args)...) == cudaSuccess) return DC_OK;
+    cudaGetLastError();                      // the status says it; the caller's next check of its own does not find it again
+    return DC_ERR_CUDA;
 }
 __device__ __forceinline__ void follow()
 {

@@ -68,6 +68,9 @@ def test_embed(api, N, V, D, dtype):
     close(out, want, want.abs() * (plain.ROUND[dtype] + 2.0 ** -23) + plain.TINY[dtype], (N, V, D))
     again = api.embed(table, ids, scale=1.7)         # no padding token: a negative id matches nothing, not even -1
     assert torch.equal(again.isnan().all(-1), (ids < 0) | (ids >= V))
+    if N:
+        lowest = torch.full((1,), -(1 << 63), dtype=torch.int64, device="cuda")
+        assert bool(api.embed(table, lowest).isnan().all())
 
 
 def test_embed_strides_and_shapes(api):
@@ -383,6 +386,27 @@ def test_vocab_loss_lowest_and_infinite_logits(api):
     w[9] = 1.0
     w[1], w[512:700] = 0, 0
     assert not bool(api.vocab_loss(h, w, t).loss[7].isfinite())
+
+
+@pytest.mark.parametrize("N", [4, 40])
+def test_vocab_loss_label_at_minus_infinity(api, N):
+    """A label whose logit is -inf: its loss is +inf, lse and the other rows are as they would be."""
+    h = normal(gen(3), N, 64, dtype=BF16)
+    h[:, 0] = 1.0
+    w = normal(gen(4), 300, 64, dtype=BF16, scale=0.1)
+    w[7] = 0
+    w[7, 0] = -INF
+    h[:, 1:] = h[:, 1:].abs() + 0.01                # no zero meets the infinity
+    w[7, 1:] = -0.5
+    t = torch.full((N,), 5, device="cuda")
+    t[2] = 7
+    loss, lse = api.vocab_loss(h, w, t)
+    assert float(loss[2]) == INF and bool(lse.isfinite().all()) and bool(loss[torch.arange(N, device="cuda") != 2].isfinite().all())
+    keep = [v for v in range(300) if v != 7]
+    _, wz, *_ = plain.vocab_loss(h, w[keep], torch.full((N,), 5, device="cuda"), -100, 1.0)
+    close(lse, wz, torch.full_like(wz, 1e-4), "lse")          # 64 terms of about 0.1: 64 2^-22, exp, log
+    dh, dw = api.vocab_loss_backward(h, w, t, lse, torch.ones(N, device="cuda"), want_dhidden=True)
+    assert bool(dw.isfinite().all())
 
 
 def test_vocab_loss_strides_types_and_accumulation(api):
