@@ -139,33 +139,20 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
     }
     __syncthreads();
 
-    // The places list_*[from_list ...] go where their token's next place is; a warp does 32 at a time.
-    auto put = [&](int32_t from_list, int32_t have) {
-        for (int32_t j0 = 0; j0 < have; j0 += 32) {
-            const bool is = j0 + lane < have;
-            const int32_t key = is ? list_key[from_list + j0 + lane] : -1;
-            const uint32_t same = __match_any_sync(~0u, key);
-            const int32_t rank = __popc(same & ((1u << lane) - 1));
-            const int32_t next = is ? hist[key] : 0;
-            __syncwarp();
-            if (is) {
-                if (rank == 0) hist[key] = next + __popc(same);
-                place[first + next + rank] = list_place[from_list + j0 + lane];
-                token[first + next + rank] = (key << log_buckets) + (int32_t)bucket;
-            }
-            __syncwarp();
-        }
-    };
-    // The same for all warps' parts of the list: only taking the tokens' next places has to go by turns.
-    auto put_in_turn = [&](int32_t have) {
+    // The first `have` places of the list go where their token's next place is: 128 of them to a warp, and only taking the next
+    // places has to go by turns.
+    auto put = [&](int32_t have) {
+        const int32_t turns = (have + kWarpList - 1) / kWarpList, mine_at = warp * kWarpList;
         int32_t key[kWarpList / 32], next[kWarpList / 32];
         uint32_t same[kWarpList / 32];
 #pragma unroll
         for (int i = 0; i < kWarpList / 32; ++i) {
-            key[i] = i * 32 + lane < have ? list_key[warp * kWarpList + i * 32 + lane] : -1;
+            const int32_t j = mine_at + i * 32 + lane;
+            key[i] = j < have ? list_key[j] : -1;
             same[i] = __match_any_sync(~0u, key[i]);
+            next[i] = 0;
         }
-        for (int w = 0; w < kSortWarps; ++w) {
+        for (int w = 0; w < turns; ++w) {
             if (w == warp)
 #pragma unroll
                 for (int i = 0; i < kWarpList / 32; ++i) {
@@ -179,13 +166,13 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
         for (int i = 0; i < kWarpList / 32; ++i) {
             const int32_t to = __shfl_sync(~0u, next[i], __ffs(same[i]) - 1) + first + __popc(same[i] & ((1u << lane) - 1));
             if (key[i] >= 0) {
-                place[to] = list_place[warp * kWarpList + i * 32 + lane];
+                place[to] = list_place[mine_at + i * 32 + lane];
                 token[to] = (key[i] << log_buckets) + (int32_t)bucket;
             }
         }
     };
-    if (kept && total <= 1024) {
-        // few: they move together first, and one warp puts them, without 32 turns
+    if (kept) {
+        // the warps' parts move together
         int32_t p[kWarpList / 32], k[kWarpList / 32];
 #pragma unroll
         for (int i = 0; i < kWarpList / 32; ++i)
@@ -195,11 +182,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
         for (int i = 0; i < kWarpList / 32; ++i)
             if (i * 32 + lane < mine) { list_place[begin + i * 32 + lane] = p[i]; list_key[begin + i * 32 + lane] = (uint16_t)k[i]; }
         __syncthreads();
-        if (warp == 0) put(0, total);
-        return;
-    }
-    if (kept) {
-        put_in_turn(mine);
+        put(total);
         return;
     }
     // more places than a warp has room for (a token that holds a large part of many): the ids again, kList places at a time
@@ -216,7 +199,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort(const int64_t *__rest
                 r += __popc(all);
             }
         __syncthreads();
-        put_in_turn(max(0, min(kWarpList, total - from - warp * kWarpList)));
+        put(min(kList, total - from));
         __syncthreads();
     }
 }
