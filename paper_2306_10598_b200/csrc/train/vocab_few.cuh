@@ -53,14 +53,6 @@ struct Few {
     float2 *part; float *hit;    // [tokens][blocks], [tokens]
 };
 
-// two (maximum, sum of exp) in powers of two joined; a maximum of -inf stands for a part without a finite logit
-__device__ __forceinline__ void join_parts(float &m, float &s, float om, float os)
-{
-    const float n = fmaxf(m, om);
-    s = (m == -INFINITY ? s : s * exp2_fast(m - n)) + (om == -INFINITY ? os : os * exp2_fast(om - n));
-    m = n;
-}
-
 template <class T, int NT>
 __global__ void __launch_bounds__(kFewThreads, 2) vocab_few(const __grid_constant__ Few a)
 {

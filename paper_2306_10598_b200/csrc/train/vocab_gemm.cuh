@@ -10,7 +10,7 @@
 // (1.22 PFLOP/s; cuBLAS, the logits alone: 914), backward 2845 us (1.16).
 //
 //   what    tile of                       rows x columns      summed over        leaves as
-//   kLoss   c h W^T                       tokens x vocab      hidden             (max, sum of exp) of each row and half tile
+//   kLoss   c h W^T                       tokens x vocab      hidden             (max, sum of exp) of each row and tile
 //   kGrad   c h W^T of a piece            tokens x vocab      hidden             g in 16 bits
 //   kBack   dW = g^T h   of the piece     vocab x hidden      tokens             dW, added to or not
 //           dh = g W     of the piece     tokens x hidden     a part of vocab    partial products in fp32
@@ -25,10 +25,10 @@ constexpr int kRowBlock = 64;               // elements of the summed dimension 
 // g of one piece of the vocabulary.  8192 x 65536 x 1024 step, us: 64 MiB 4190, 128 MiB 4120, 256 MiB 4070, 512 MiB 3990, 1 GiB 3950
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
 constexpr int kStageBytes = 2 * 128 * 64 * 2;
-constexpr int kTcThreads = 384;             // warp 0 copies, warp 1 multiplies, warp 2 has the tensor memory, warps 4-11 take tiles out
 constexpr int kMaxParts = 16;
 
 enum What { kLoss, kGrad, kBack };
+constexpr int kTcThreads = 384;             // warp 0 copies, warp 1 multiplies, warp 2 has the tensor memory, warps 4-11 take tiles out
 // kBack passes its tiles through shared memory, 32 x 32 to a warp, so that it has room for a stage less
 constexpr int kPitch = 36;                  // floats to a row there: 16-byte accesses of a row each and along rows meet no bank twice
 __host__ __device__ constexpr int stages_of(int what) { return what == kBack ? 5 : 6; }
@@ -156,28 +156,46 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __half)
     return *reinterpret_cast<const uint32_t *>(&x);
 }
 
-// Running maximum and sum of exp over 32 more logits (in powers of two).  Where nothing finite has been seen the maximum
-// stays -inf and the sum 0; a NaN reaches the sum, a +inf makes it NaN.
+// Running maximum and sum of exp over 32 more logits c v (in powers of two), of which `valid` count.  Where nothing finite has
+// been seen the maximum stays -inf and the sum 0; a NaN reaches the sum, a +inf makes it NaN.
+template <bool ALL>
 __device__ __forceinline__ void online(const float (&v)[32], int32_t valid, float c, float &m, float &s)
 {
-    float z[32];
-    float t0 = m, t1 = -INFINITY;
+    float r0, r1;
+    if (c >= 0.0f) {
+        r0 = r1 = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        z[i] = i < valid ? v[i] * c : -INFINITY;
-        z[i + 1] = i + 1 < valid ? v[i + 1] * c : -INFINITY;
-        t0 = fmaxf(t0, z[i]);
-        t1 = fmaxf(t1, z[i + 1]);
-    }
-    const float top = fmaxf(t0, t1), ref = top == -INFINITY ? 0.0f : top;
-    float a = s * exp2_fast(m - ref), b = 0.0f;             // m = -inf: 0 times 0
+        for (int i = 0; i < 32; i += 2) {
+            r0 = fmaxf(r0, ALL || i < valid ? v[i] : -INFINITY);
+            r1 = fmaxf(r1, ALL || i + 1 < valid ? v[i + 1] : -INFINITY);
+        }
+        r0 = fmaxf(r0, r1);
+    } else {
+        r0 = r1 = INFINITY;
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        a += exp2_fast(z[i] - ref);
-        b += exp2_fast(z[i + 1] - ref);
+        for (int i = 0; i < 32; i += 2) {
+            r0 = fminf(r0, ALL || i < valid ? v[i] : INFINITY);
+            r1 = fminf(r1, ALL || i + 1 < valid ? v[i + 1] : INFINITY);
+        }
+        r0 = fminf(r0, r1);
     }
+    const float top = fmaxf(m, r0 * c), ref = top == -INFINITY ? 0.0f : top;
+    const uint64_t cc = pair_of(c, c), less = pair_of(-ref, -ref);
+    uint64_t a = pair_of(s * exp2_fast(m - ref), 0.0f), b = pair_of(0.0f, 0.0f);   // m = -inf: 0 times 0
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+        float e[4];
+        split(fma_pair(pair_of(v[i], v[i + 1]), cc, less), e[0], e[1]);
+        split(fma_pair(pair_of(v[i + 2], v[i + 3]), cc, less), e[2], e[3]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] = ALL || i + k < valid ? exp2_fast(e[k]) : 0.0f;
+        a = add_pair(a, pair_of(e[0], e[1]));
+        b = add_pair(b, pair_of(e[2], e[3]));
+    }
+    float x, y;
+    split(add_pair(a, b), x, y);
     m = top;
-    s = a + b;
+    s = x + y;
 }
 
 // 32 x 32 results of a warp, a row to a thread, to rows of `to` that are `stride` apart: times `f`, added or not.  They change
@@ -237,6 +255,9 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
     constexpr int kStages = stages_of(WHAT);
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t full[kStages], empty[kStages], ready[2], taken[2];
+    // kLoss: what the second of two warps with the same rows found in its columns, that it has written that, that the first has read it
+    __shared__ float2 found[2][WHAT == kLoss ? 128 : 1];
+    __shared__ uint64_t written[4][2], joined[4][2];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up_at;
     volatile int *gave_up = &gave_up_at;
@@ -253,6 +274,7 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
         gave_up_at = 0;
         for (int i = 0; i < kStages; ++i) { bar_init(smem_u32(&full[i]), 1); bar_init(smem_u32(&empty[i]), 1); }
         for (int i = 0; i < 2; ++i) { bar_init(smem_u32(&ready[i]), 1); bar_init(smem_u32(&taken[i]), 16); }
+        for (int i = 0; WHAT == kLoss && i < 8; ++i) { bar_init(smem_u32(&written[i >> 1][i & 1]), 1); bar_init(smem_u32(&joined[i >> 1][i & 1]), 1); }
         bar_init_visible();
     }
     if (warp == 2) tmem_alloc(smem_u32(&tmem_at), 512);
@@ -321,7 +343,7 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
         }
     } else if (warp >= 4) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        uint32_t buf = 0, buf_phase = 0;
+        uint32_t buf = 0, buf_phase = 0, turn = 0, turn_phase = 0;
         for (int32_t u = pair; u < units.count && !__any_sync(~0u, *gave_up); u += pairs) {
             const Unit t = units.get(u, p);
             const int32_t row = t.m + (int32_t)rank * 128 + quarter * 32 + lane;
@@ -343,22 +365,13 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
             __syncwarp();
             // rows that nothing is kept of are not taken out; g has zeros up to the next kRowBlock, which dW is summed over
             const int32_t row0 = row - lane, rows_out = WHAT == kGrad ? (units.rows + kRowBlock - 1) / kRowBlock * kRowBlock : WHAT == kBack && t.dw ? p.V : units.rows;
-#pragma unroll 1
-            for (int j = 0; j < (row0 < rows_out ? 4 : 0); ++j) {
+            auto take = [&](int j, float (&v)[32]) {
                 const int32_t col = c0 + j * 32;
-                float v[32];
-                if (t.blocks > 0) {
-                    tmem_load(from + j * 32, v);
-                    tmem_load_done();
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = 0.0f;
-                }
                 if (WHAT == kLoss) {
                     const int32_t valid = p.V - col;
-                    if (valid <= 0) break;
-                    if (valid >= 32) online(v, 32, p.scale, m, s);
-                    else online(v, valid, p.scale, m, s);
+                    if (valid <= 0) return;
+                    if (valid >= 32) online<true>(v, valid, p.scale, m, s);
+                    else online<false>(v, valid, p.scale, m, s);
                     const int32_t l = label - col;
                     if (__any_sync(~0u, l >= 0 && l < 32)) {
 #pragma unroll
@@ -366,8 +379,13 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
                     }
                 } else if (WHAT == kGrad) {
                     const int32_t valid = row < units.rows ? p.V - col : 0, l = label - col;
+                    const uint64_t cc = pair_of(p.scale, p.scale), less = pair_of(-lse2, -lse2), ff = pair_of(f, f);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = exp2_fast(fmaf(v[i], p.scale, -lse2)) * f;
+                    for (int i = 0; i < 32; i += 2) {
+                        float x, y;
+                        split(fma_pair(pair_of(v[i], v[i + 1]), cc, less), x, y);
+                        split(mul_pair(pair_of(exp2_fast(x), exp2_fast(y)), ff), v[i], v[i + 1]);
+                    }
                     if (__any_sync(~0u, l >= 0 && l < 32)) {
                         float g = 0.0f;
                         if (l >= 0 && l < 32) {
@@ -394,19 +412,63 @@ vocab_product(const __grid_constant__ CUtensorMap a, const __grid_constant__ CUt
                     if (t.dw) {
                         const int32_t r = min(32, p.V - row0), c = p.D - col;
                         const int64_t at = (int64_t)row0 * p.dw_stride + col;
-                        if (c <= 0) break;
+                        if (c <= 0) return;
                         if (p.dw_f32) put_tile(room, v, (float *)p.dw + at, p.dw_stride, r, c, unscale, p.dw_add, p.dw_wide);
                         else put_tile(room, v, (T *)p.dw + at, p.dw_stride, r, c, unscale, p.dw_add, p.dw_wide);
                     } else {
                         const int32_t r = min(32, units.rows - row0);
-                        if (col >= p.Dp || (t.blocks == 0 && !p.first)) break;
+                        if (col >= p.Dp || (t.blocks == 0 && !p.first)) return;
                         put_tile(room, v, p.acc + ((int64_t)t.part * units.rows + row0) * p.Dp + col, p.Dp, r, 32, 1.0f, !p.first, true);
                     }
                 }
+            };
+            if (WHAT == kLoss && row0 < rows_out) {
+                // The next 32 columns are on their way while these are worked on: 8192 x 32768 x 64, which is nothing but taking
+                // out, 145 us and without 157.  (Twice the warps without: 134, but 2 % more at hidden 512 and above, where power
+                // decides.)  The backward's tiles wait for their stores, and lose 1 to 3 % by it.
+                float v[2][32];
+                tmem_load(from, v[0]);
+#pragma unroll 1
+                for (int j = 0; j < 4; j += 2) {
+                    tmem_load_done(v[0]);
+                    tmem_load(from + j * 32 + 32, v[1]);
+                    take(j, v[0]);
+                    __syncwarp();
+                    tmem_load_done(v[1]);
+                    if (j == 0) tmem_load(from + 64, v[0]);
+                    take(j + 1, v[1]);
+                    __syncwarp();
+                }
+            } else if (row0 < rows_out) {
+#pragma unroll 1
+                for (int j = 0; j < 4; ++j) {
+                    float v[32] = {};
+                    __syncwarp();
+                    if (t.blocks > 0) {
+                        tmem_load(from + j * 32, v);
+                        tmem_load_done(v);
+                    }
+                    take(j, v);
+                }
             }
-            if (WHAT == kLoss && row < units.rows) {
-                p.part[(int64_t)row * p.part_pitch + (c0 >> 7)] = make_float2(m, s);
+            if (WHAT == kLoss && row0 < rows_out) {
                 if (label >= c0 && label < c0 + 128) p.hit[row] = at_label * (p.scale * 0.6931471805599453f);
+                const uint32_t here = smem_u32(&written[quarter][turn]), read = smem_u32(&joined[quarter][turn]);
+                if (half > 0) {
+                    if (!__all_sync(~0u, bar_wait(read, turn_phase ^ 1, gave_up, 16u))) break;
+                    found[turn][quarter * 32 + lane] = make_float2(m, s);
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(here);
+                } else {
+                    if (!__all_sync(~0u, bar_wait(here, turn_phase, gave_up, 16u))) break;
+                    const float2 o = found[turn][quarter * 32 + lane];
+                    join_parts(m, s, o.x, o.y);
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(read);
+                    if (row < units.rows) p.part[(int64_t)row * p.part_pitch + t.n / kTileN] = make_float2(m, s);
+                }
+                turn ^= 1;
+                turn_phase ^= turn == 0;
             }
             if (t.blocks > 0) {
                 tc_before_sync();

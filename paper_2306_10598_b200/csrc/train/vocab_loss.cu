@@ -247,7 +247,7 @@ inline Plan make_plan(void *base, int64_t N, int64_t V, int64_t D, const void *w
     if (p.copy_weight) p.weight = take((size_t)V * p.Dp * 2);
     if (!backward) {
         p.hit = (float *)take(p.Lp * 4);
-        const size_t parts = (size_t)p.Lp * p.tiles_v * 2, of_few = (size_t)kFewTokens * kMostFewBlocks;
+        const size_t parts = (size_t)p.Lp * p.tiles_v, of_few = (size_t)kFewTokens * kMostFewBlocks;
         p.part = (float2 *)take((parts > of_few ? parts : of_few) * 8);
     } else {
         p.row_lse = (float *)take(p.Lp * 4);
@@ -316,10 +316,10 @@ int forward(Gather g, const Plan &p, const void *weight, int64_t ws, float *loss
     if (!tensor_map(&a, p.rows, bf, p.Dp, p.Lp, p.Dp, 128) || !tensor_map(&b, p.copy_weight ? p.weight : weight, bf, g.D, g.V, p.copy_weight ? p.Dp : ws, 128))
         return DC_ERR_CUDA;
     if (int e = gather<T>(g, p, &weight, &ws, st)) return e;
-    q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.part = p.part; q.hit = p.hit; q.part_pitch = 2 * p.tiles_v;
+    q.head = p.head; q.label = p.label; q.scale = g.logit_scale * 1.4426950408889634f; q.part = p.part; q.hit = p.hit; q.part_pitch = p.tiles_v;
     q.V = (int32_t)g.V; q.D = g.D; q.Dp = p.Dp;
     if (int e = launch_units<T, kLoss>(p.Lp / kTileM * p.tiles_v, pairs, a, b, a, b, q, st)) return e;
-    return launch(vocab_join, dim3((unsigned)ceil_div(g.N, 8)), 256, 0, st, p.head, p.row_of, p.part, p.hit, p.row_hit, 2 * p.tiles_v, loss, lse);
+    return launch(vocab_join, dim3((unsigned)ceil_div(g.N, 8)), 256, 0, st, p.head, p.row_of, p.part, p.hit, p.row_hit, p.tiles_v, loss, lse);
 }
 
 template <class T>
