@@ -35,9 +35,11 @@ inline bool on(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p)
 // rows of a matrix whose starts all fall on `a`-byte boundaries
 inline bool rows_on(const void *p, int64_t stride, int eb, size_t a) { return on(p, a) && (size_t)(stride * eb) % a == 0; }
 
-// Kernels follow each other, those of one call and of calls in a row, with programmatic dependent launch: the next one may start, and set itself up, while
-// the last blocks of the one before still run, and waits in follow() until that one is done and its writes are visible.  Every
-// kernel calls it before it touches global memory, so all that went before in the stream is done too.
+// Kernels follow each other, those of one call and of calls in a row, with programmatic dependent launch: the next one may start,
+// and set itself up, while this one runs, and waits in follow() until this one is done and its writes are visible.  Every kernel
+// calls it before it touches global memory, so all that went before in the stream is done too.  The next one is let in only after
+// the wait, so that two kernels at most are on the device: let in before it, whole chains were, and under a kernel trace the device
+// did not get to their end.  Without all this a step of seven kernels (251 x 5003 x 129) takes 58.8 us instead of 42.7.
 template <class... P, class... A> int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const A &...args)
 {
     cudaLaunchConfig_t c = {};
@@ -56,8 +58,8 @@ template <class... P, class... A> int launch(void (*kernel)(P...), dim3 grid, in
 }
 __device__ __forceinline__ void follow()
 {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 // A pack of adjacent elements of a row: 16 bytes where rows start on 16-byte boundaries, one element otherwise.
