@@ -25,7 +25,7 @@ constexpr int kRowBlock = 64;               // elements of the summed dimension 
 // g of one piece of the vocabulary.  8192 x 65536 x 1024 step, us: 64 MiB 4190, 128 MiB 4120, 256 MiB 4070, 512 MiB 3990, 1 GiB 3950
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
 constexpr int kStageBytes = 2 * 128 * 64 * 2;
-constexpr int kMaxParts = 16;
+constexpr int kMaxParts = 32;               // one to a lane, see parts_of.  Backward of 100 x 45976 x 512: with 16 at most 69.5 us, with 32 65.4
 
 enum What { kLoss, kGrad, kBack };
 constexpr int kTcThreads = 384;             // warp 0 copies, warp 1 multiplies, warp 2 has the tensor memory, warps 4-11 take tiles out
@@ -43,7 +43,8 @@ struct Head {
 
 // In how many parts of the vocabulary dh is summed: few tiles of dh leave most of the GPU idle, many parts cost fp32 traffic.
 // A pair of CTAs c takes units c, c + pairs, ...: first the tiles of dW (rb blocks each), then those of dh; the parts that give
-// the shortest longest list are taken.  Each unit is charged kUnitCost blocks for taking its tile out.  The tiles of dW count
+// the shortest longest list are taken.  Each unit is charged kUnitCost blocks for taking its tile out, and four parts one block for
+// being joined (100 x 8000 x 256, backward: without that 28.2 us, with it 27.4).  The tiles of dW count
 // whether dW is asked for or not, so that dh has the same bits either way.
 constexpr uint32_t kUnitCost = 6;
 __device__ inline uint32_t up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
@@ -54,7 +55,7 @@ __device__ inline int32_t parts_of(uint32_t rows, uint32_t D, uint32_t vocab_blo
     const uint32_t nw = up(vocab_blocks, kTileM / kRowBlock) * td, q = nw / pairs, r = nw % pairs;
     const uint32_t len = up(vocab_blocks, s), cost = len + kUnitCost, n = up(rows, kTileM) * td * s, q2 = n / pairs, r2 = n % pairs;
     const uint32_t dw = r ? rb : 0, dh = r2 ? cost : 0, extra = r + r2 > pairs ? dw + dh : max(dw, dh);
-    uint64_t total = (uint64_t)q * rb + (uint64_t)q2 * cost + extra;
+    uint64_t total = (uint64_t)q * rb + (uint64_t)q2 * cost + extra + s / 4;
     // s parts of `len` blocks have to leave none empty, and their sums have to fit
     if (s > 1 && (s > kMaxParts || s > vocab_blocks || (int64_t)s * rows > acc_rows || up(vocab_blocks, len) != s)) total = ~0ull;
     uint32_t best = s;
