@@ -4,6 +4,7 @@
 // can hold several per cent of all places.  Places are grouped by token first (embed_sort), and the sum then runs over
 // equal tiles of the grouped list, whatever the tokens are: a token that is spread over several tiles leaves one partial
 // sum per tile, which embed_join adds in order.  No element is added to twice in a call, so two calls give the same bits.
+// Up to kFewPlaces places need no grouping (embed_few).
 #include "train_common.cuh"
 
 namespace dct {
@@ -403,6 +404,127 @@ __global__ void __launch_bounds__(512) embed_join(const int32_t *__restrict__ to
     }
 }
 
+// ---- few places: one launch ---------------------------------------------------------------------------------------------------
+
+// A warp takes (place, 512 bytes' worth of columns).  Every block has the tokens of all places in shared memory; a warp whose token
+// occurs earlier has nothing to do, the others add up the rows of all their token's places in order, the whole block together where
+// they are more than kAlone: each warp a run of them, joined in order.  Blocks from sum_blocks on write zeros to the rows of `range`
+// tokens each, but for those that occur.
+// Bound by the few steps that follow one another.  Against three launches, added to fp32, us: 64 places x 256 14.5 -> 5.0, 256 x 69
+// 24.5 -> 5.5 to 8, 512 x 1024 16.4 -> 6.5 (all of one token 11.3 -> 12.7); 1024 x 1024 17.8 -> 11.9, but of one token 15.2 -> 22.8.
+constexpr int kFewPlaces = 512, kFewRange = 4096, kFewWarps = 8, kAlone = 16;
+
+template <class T, class O, int V>
+__global__ void __launch_bounds__(32 * kFewWarps) embed_few(const T *__restrict__ dout, int64_t ds, const int64_t *__restrict__ ids, int32_t N, int64_t vocab,
+                                                            int64_t pad, int64_t D, float scale, O *__restrict__ dtable, int64_t ts, bool accumulate,
+                                                            int64_t sum_blocks, int32_t range)
+{
+    constexpr int K = kPacks<T, V>, U = 8;
+    __shared__ int32_t token[kFewPlaces];
+    __shared__ uint16_t places[kFewWarps][kFewPlaces];
+    __shared__ uint32_t occurs[kFewRange / 32];
+    __shared__ int32_t count[kFewWarps];
+    __shared__ float others[kFewWarps][K * V][32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool sums = blockIdx.x < sum_blocks;
+    const int64_t v0 = sums ? 0 : (blockIdx.x - sum_blocks) * (int64_t)range, v1 = min(vocab, v0 + range);
+    follow();
+    if (tid < kFewRange / 32) occurs[tid] = 0;
+    __syncthreads();
+    for (int32_t i = tid; i < N; i += 32 * kFewWarps) {
+        const uint64_t x = (uint64_t)ids[i];
+        const bool is = x < (uint64_t)vocab && x != (uint64_t)pad;
+        if (sums) token[i] = is ? (int32_t)x : -1;
+        else if (is && (int64_t)x >= v0 && (int64_t)x < v1) atomicOr(&occurs[(x - v0) >> 5], 1u << ((x - v0) & 31));
+    }
+    __syncthreads();
+    if (!sums) {
+        for (int64_t v = v0 + warp; v < v1; v += kFewWarps)
+            if (!(occurs[(v - v0) >> 5] >> ((v - v0) & 31) & 1)) zero_row(dtable + v * ts, D, lane);
+        return;
+    }
+    const int32_t eights = (N + kFewWarps - 1) / kFewWarps, n = (int32_t)(blockIdx.x % eights) * kFewWarps + warp;
+    const int64_t c = (int64_t)(blockIdx.x / eights) * (32 * K * V) + lane * V;
+    auto add = [&](float (&sum)[K][V], const uint16_t *list, int32_t count) {
+        for (int32_t j0 = 0; j0 < count; j0 += U) {
+            Pack<T, V> x[U][K];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    x[u][k] = Pack<T, V>{};
+                    if (j0 + u < count && c + k * (32 * V) < D) x[u][k] = *reinterpret_cast<const Pack<T, V> *>(dout + list[j0 + u] * ds + c + k * (32 * V));
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum[k][i] += to_f(x[u][k].v[i]);
+        }
+    };
+    auto finish = [&](const float (&sum)[K][V], int32_t tok) {
+        O *row = dtable + (int64_t)tok * ts + c;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (c + k * (32 * V) < D) finish_row<O, V>(row + k * (32 * V), sum[k], scale, accumulate);
+    };
+    const int32_t tok = n < N ? token[n] : -1;
+    int32_t have = 0;
+    for (int32_t i0 = 0; tok >= 0 && i0 < N; i0 += 32) {
+        const int32_t i = i0 + lane;
+        const bool is = i < N && token[i] == tok;
+        const uint32_t all = __ballot_sync(~0u, is);
+        if (all && have == 0 && i0 + __ffs(all) - 1 < n) break;              // another warp's
+        if (is) places[warp][have + __popc(all & ((1u << lane) - 1))] = (uint16_t)i;
+        have += __popc(all);
+    }
+    __syncwarp();
+    if (have > 0 && have <= kAlone) {
+        float sum[K][V] = {};
+        add(sum, places[warp], have);
+        finish(sum, tok);
+    }
+    if (lane == 0) count[warp] = have;
+    if (!__syncthreads_or(have > kAlone)) return;
+    for (int w = 0; w < kFewWarps; ++w) {
+        if (count[w] <= kAlone) continue;
+        const int32_t each = (count[w] + kFewWarps - 1) / kFewWarps, from = min(warp * each, count[w]);
+        float sum[K][V] = {};
+        add(sum, places[w] + from, min(each, count[w] - from));
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) others[warp][k * V + i][lane] = sum[k][i];
+        __syncthreads();
+        if (warp == w) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    sum[k][i] = 0.0f;
+                    for (int q = 0; q < kFewWarps; ++q) sum[k][i] += others[q][k * V + i][lane];
+                }
+            finish(sum, tok);
+        }
+        __syncthreads();
+    }
+}
+
+template <class T, class O, int V>
+int few_launch(const void *dout, int64_t ds, const int64_t *ids, int64_t N, int64_t vocab, int64_t pad, int64_t D, float scale, void *dtable, int64_t ts,
+               bool accumulate, cudaStream_t st)
+{
+    const int32_t chunks = (int32_t)ceil_div(D, 32 * V * kPacks<T, V>);
+    const int64_t sums = ceil_div(N, kFewWarps) * chunks, most = (int64_t)sm_count() * 4, rows = ceil_div(vocab, kFewWarps);
+    int64_t range = ceil_div(vocab, rows < most ? rows : most), zeros = 0;
+    if (range > kFewRange) range = kFewRange;
+    if (!accumulate) zeros = ceil_div(vocab, range);
+    if (sums + zeros > INT32_MAX) return DC_ERR_RANGE;
+    return launch(embed_few<T, O, V>, dim3((unsigned)(sums + zeros)), 32 * kFewWarps, 0, st, (const T *)dout, ds, ids, (int32_t)N, vocab, pad, D, scale,
+                  (O *)dtable, ts, accumulate, sums, (int32_t)range);
+}
+
 struct SortPlan { int32_t log_buckets; int32_t keys; };
 inline SortPlan sort_plan(int64_t V)
 {
@@ -511,14 +633,18 @@ extern "C" int dc_embed_backward(const void *dout, int64_t dout_stride, int32_t 
         return cudaMemset2DAsync(dtable, (size_t)dtable_stride * ob, 0, (size_t)D * ob, (size_t)V, st) == cudaSuccess ? DC_OK : DC_ERR_CUDA;
     }
     if (sm_count() == 0) return DC_ERR_CUDA;
-    const Work w = carve(workspace, N, V, D);
-    const SortPlan p = sort_plan(V);
-    if (int e = launch(embed_sort, dim3(1u << p.log_buckets), kSortThreads, (size_t)p.keys * 4, st, ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token,
-                       w.live, accumulate ? nullptr : w.occurs)) return e;
     // packs of 16 bytes of dout, and of as many elements of dtable
     const int W = 16 / eb;
     const bool wide = D % W == 0 && rows_on(dout, dout_stride, eb, (size_t)(W * eb)) && rows_on(dtable, dtable_stride, ob, (size_t)(W * ob));
-#define DCT_SUM(T, O, V_) backward_launch<T, O, V_>(dout, dout_stride, N, V, D, scale, dtable, dtable_stride, accumulate != 0, w, st)
+    const bool few = N <= kFewPlaces;
+    const Work w = carve(workspace, N, V, D);
+    const SortPlan p = sort_plan(V);
+    if (!few)
+        if (int e = launch(embed_sort, dim3(1u << p.log_buckets), kSortThreads, (size_t)p.keys * 4, st, ids, (int32_t)N, V, pad_id, p.log_buckets, w.place, w.token,
+                           w.live, accumulate ? nullptr : w.occurs)) return e;
+#define DCT_SUM(T, O, V_)                                                                                                                      \
+    (few ? few_launch<T, O, V_>(dout, dout_stride, ids, N, V, pad_id, D, scale, dtable, dtable_stride, accumulate != 0, st)                     \
+         : backward_launch<T, O, V_>(dout, dout_stride, N, V, D, scale, dtable, dtable_stride, accumulate != 0, w, st))
     if (dtype == DC_F32) return wide ? DCT_SUM(float, float, 4) : DCT_SUM(float, float, 1);
     if (dtype == DC_BF16) {
         if (dtable_dtype == DC_F32) return wide ? DCT_SUM(__nv_bfloat16, float, 8) : DCT_SUM(__nv_bfloat16, float, 1);
