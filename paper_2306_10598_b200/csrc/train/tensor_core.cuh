@@ -37,7 +37,7 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // For a barrier that hands tensor memory on and nothing else: the fences of tcgen05 order that, and an arrival that released all
-// of a thread's memory to the cluster would wait until its stores had landed (8192 x 32768 x 256: forward 166 us, with such arrivals 208; backward 454 and 505)
+// of a thread's memory to the cluster would wait until its stores had landed (8192 x 32768 x 256, backward: 454 us, with such arrivals 505)
 __device__ __forceinline__ void bar_arrive_in_cluster(uint32_t cluster_bar)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");

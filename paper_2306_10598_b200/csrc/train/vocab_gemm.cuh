@@ -4,10 +4,10 @@
 // both operands (64 of the summed dimension at a time) into a ring in shared memory by bulk tensor copies, one thread of the
 // pair issues the products into tensor memory, and eight warps of each CTA take finished tiles from there.  Tensor memory
 // holds two tiles, so the products of one run while the other is taken out: exp, maxima and sums hide behind the products.
-// Measured with all rows labelled, a tile of 256 x 256 costs a pair 711-733 cycles for each 64 of the summed dimension (512 at the
-// tensor cores' rate) and 1600 besides.  What bounds it is what L2 delivers, 64 KB for those 64 (9.3-10.8 TB/s over the GPU), and
-// with that the 1000 W limit: the share of the tensor peak falls as the clock rises.  8192 x 65536 x 1024 bf16: forward 899 us
-// (1.22 PFLOP/s; cuBLAS, the logits alone: 914), backward 2845 us (1.16).
+// 8192 x 65536 x 1024 bf16, all rows labelled: forward 855 us (1.29 PFLOP/s; cuBLAS, the logits alone: 914), backward 2767 us
+// (1.19).  A tile of 256 x 256 then costs a pair 730 cycles for each 64 of the summed dimension, all else included (512 at the
+// tensor cores' rate).  What bounds it is what L2 delivers, 64 KB for those 64 (9.3-10.6 TB/s over the GPU), and with that the
+// 1000 W limit: the share of the tensor peak falls as the clock rises.  Below a hidden size of 512 taking the tiles out decides.
 //
 //   what    tile of                       rows x columns      summed over        leaves as
 //   kLoss   c h W^T                       tokens x vocab      hidden             (max, sum of exp) of each row and tile
